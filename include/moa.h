@@ -333,6 +333,127 @@ moa_status moa_debug_kernel_stats(moa_engine* e, moa_kernel_stats* out);
  * 1 GiB; ESTATE: plan-only engine or unusable engine; EHIP: runtime error. */
 moa_status moa_debug_measure_peaks(moa_engine* e, double* read_bytes_per_s, double* mfma_flops_per_s);
 
+/* ---- operators on the caller's own tensors ----
+ *
+ * What a layer does around its paged cache, and what the head says about a
+ * token, for callers that keep their own tensors and cache pools; the engine's
+ * steps launch the same kernels (MOA_FLAG_KV_INT4, MOA_FLAG_QK_NORM,
+ * moa_request_scores).
+ *
+ * Every pointer but cfg and bytes is device memory of hip_stream's device,
+ * which must be the current device; the work is enqueued on hip_stream and
+ * nothing is allocated, copied to the host or waited for, so the calls can be
+ * captured into a graph. Matrices are row-major; a stride is the elements
+ * from one row to the next (at least the row's width, any alignment of the
+ * element). Sizes and the values of cfg are checked (MOA_EINVAL); index
+ * tensors are read on the device, where an entry that is out of range is
+ * skipped as each call states. A call of zero rows does nothing. workspace
+ * (256-byte aligned, MOA_ENOMEM if it is smaller than the *_bytes call says)
+ * is scratch of one call: calls that may overlap on the device, two graphs
+ * that replay at once among them, need one each. MOA_EHIP: the launch failed.
+ */
+
+/* How a pool holds K and V. */
+enum { MOA_KV_F32 = 0, MOA_KV_BF16 = 1, MOA_KV_INT4 = 2 };
+
+/* A paged pool: [n_layers][num_blocks][n_kv_heads] cells of 16 positions of
+ * one head (head_dim D = 64 or 128). n_heads query heads share the KV heads;
+ * n_heads / n_kv_heads is 1, 2, 4 or 8. The pool is 16-byte aligned.
+ *   F32, BF16: a cell is K [16][D], then V [16][D].
+ *   INT4: a cell is 16 D + 128 bytes:
+ *     K codes [16][D / 2]: byte i of a position has dims 2 i (low four bits) and 2 i + 1;
+ *     V codes [D / 2][16]: byte i of a position has dims i (low four bits) and i + D / 2;
+ *     K scales [16], V scales [16]: bf16 pairs (s, m), s in the lower half of the word.
+ *   Code c stands for m + s c. A row (a position's K or V of one head, as
+ *   float32) is stored with m = bf16(min), s = bf16((max - min) / 15) and
+ *   c = (x - m) / s rounded half to even and clamped to 0 .. 15 (0 where s = 0).
+ *   A row with a NaN, an infinity or a range past float32 has s = NaN, so all
+ *   of it stands for NaN. */
+typedef struct {
+  int32_t kind, n_layers, num_blocks, n_heads, n_kv_heads, head_dim;
+} moa_kv_cfg;
+
+/* Bytes of a pool. EINVAL: inconsistent cfg. */
+moa_status moa_kv_bytes(const moa_kv_cfg* cfg, size_t* bytes);
+
+/* Norms of the queries and keys of each head, the position rotation and the
+ * append to the cache in one pass. qkv [n_rows] rows of (n_heads + 2
+ * n_kv_heads) * D elements (queries, keys, values) of `type` (MOA_F32 or
+ * MOA_BF16). Row r is position p = row_pos[r] of sequence row_seq[r], whose
+ * position p lies in block tables[row_seq[r]][p / 16], slot p % 16 (tables:
+ * [n_seqs][table_len] block ids).
+ *   q_gain, k_gain (both or neither NULL): [D] of gain_type; each query and
+ *     key head becomes x / sqrt(mean(x^2) + eps) * gain.
+ *   rope (or NULL: no rotation): [rope_len][D / 2] pairs (cos, sin); pairs
+ *     (i, i + D / 2) of queries and keys are turned by row p.
+ *   q: [n_rows][n_heads][D] of `type`, written; keys and values are written
+ *     to `layer` of kv. The keys of a 4-bit pool are computed in 64 bits and
+ *     rounded to float32 once, so that no code hangs on the order of a sum.
+ * A row with p < 0 (padding) or, with rope, p >= rope_len is left alone; one
+ * whose sequence, table entry or block is out of range has its q written and
+ * nothing cached. The rows' positions must be distinct: of two rows that name
+ * one slot, the bytes of either may stay. */
+moa_status moa_kv_append(const moa_kv_cfg* cfg, void* kv, int32_t layer, const void* qkv, int32_t type,
+                         int64_t qkv_stride, int32_t n_rows, const int32_t* row_seq, const int32_t* row_pos,
+                         const int32_t* tables, int32_t n_seqs, int32_t table_len, const float* rope,
+                         int32_t rope_len, const void* q_gain, const void* k_gain, int32_t gain_type, float eps,
+                         void* q, void* hip_stream);
+
+/* What the cache holds at given positions: k, v [n_rows][n_kv_heads][D],
+ * float32 from an F32 pool, else bf16 (4-bit values rounded to it). Rows
+ * that are out of range (position, sequence, table entry, block) read as 0. */
+moa_status moa_kv_read(const moa_kv_cfg* cfg, const void* kv, int32_t layer, int32_t n_rows, const int32_t* row_seq,
+                       const int32_t* row_pos, const int32_t* tables, int32_t n_seqs, int32_t table_len, void* k,
+                       void* v, void* hip_stream);
+
+/* Attention of decode rows over a 4-bit pool: row r's query heads see keys
+ * [0, c), c = min(row_ctx[r], max_ctx), of sequence row_seq[r], and out[r]
+ * [n_heads][D] = softmax(scale * q . k) . v. q rows (n_heads * D elements) and
+ * out are of `type`; sums, the softmax and its statistics are float32, q and
+ * the probabilities enter the products with at least 16 significant bits. A
+ * row with c <= 0 or a sequence out of range is 0 (rows of one call may share
+ * a sequence and may see fewer keys than it has). max_ctx bounds the work
+ * (1 <= max_ctx <= 16 table_len): the keys of long rows are split among
+ * workgroups and joined in a fixed order, in splits that depend on nothing
+ * but the row. Block ids out of range are read as the pool's last block.
+ * EINVAL too: the pool is not INT4. */
+moa_status moa_kv_attend_bytes(const moa_kv_cfg* cfg, int32_t n_rows, int32_t max_ctx, size_t* bytes);
+moa_status moa_kv_attend(const moa_kv_cfg* cfg, const void* kv, int32_t layer, const void* q, int32_t type,
+                         int64_t q_stride, int32_t n_rows, const int32_t* row_seq, const int32_t* row_ctx,
+                         const int32_t* tables, int32_t n_seqs, int32_t table_len, int32_t max_ctx, float scale,
+                         void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Causal attention of prompt chunks over a 4-bit pool: chunk i is rows
+ * [chunk_start[i], chunk_start[i + 1]) (chunk_start: n_chunks + 1 ascending
+ * entries, within [0, n_rows]) and its last row is position chunk_ctx[i] - 1 of
+ * the sequence of tables[i]; a row at position p sees keys [0, p], and one at
+ * p < 0 is 0. Rows in no chunk are left as they were. Otherwise as
+ * moa_kv_attend, with chunk_ctx[i] <= max_ctx (a chunk past it is clamped to
+ * end at max_ctx). Chunks of any lengths may stand side by side, empty ones
+ * too; single rows are what moa_kv_attend is for. */
+moa_status moa_kv_attend_chunks_bytes(const moa_kv_cfg* cfg, int32_t n_rows, int32_t n_chunks, int32_t max_ctx,
+                                      size_t* bytes);
+moa_status moa_kv_attend_chunks(const moa_kv_cfg* cfg, const void* kv, int32_t layer, const void* q, int32_t type,
+                                int64_t q_stride, int32_t n_rows, const int32_t* chunk_start,
+                                const int32_t* chunk_ctx, const int32_t* tables, int32_t n_chunks,
+                                int32_t table_len, int32_t max_ctx, float scale, void* out, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
+
+/* Log probabilities of given tokens under rows of logits [n_rows][vocab] of
+ * `type`, with the entropy of each row and its top_k (0 .. MOA_MAX_TOP, at
+ * most vocab) likeliest tokens:
+ *   logprob[r] = log softmax(logits[r])[tokens[r]]   (NaN for a token outside [0, vocab));
+ *   entropy[r] = -sum p log p, natural units         (an impossible token, logit -inf, adds 0);
+ *   top_ids, top_logprobs [n_rows][top_k], by falling logit, ties to the lower id (NULL when top_k is 0).
+ * All results are float32 (ids int32), summed in float32. A row that holds a
+ * NaN or +inf, or nothing above -inf, has NaN for every probability; its
+ * top_ids still name top_k distinct tokens, the order of NaNs being last. */
+enum { MOA_MAX_TOP = 32 };
+moa_status moa_score_tokens_bytes(int32_t n_rows, int32_t vocab, int32_t top_k, size_t* bytes);
+moa_status moa_score_tokens(const void* logits, int32_t type, int64_t stride, int32_t n_rows, int32_t vocab,
+                            const int32_t* tokens, float* logprob, float* entropy, int32_t top_k, int32_t* top_ids,
+                            float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

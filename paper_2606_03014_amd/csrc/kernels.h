@@ -184,4 +184,77 @@ hipError_t scratch_address(void** out);
 hipError_t launch_peak_read(hipStream_t st, const void* p, size_t bytes, unsigned* sink, int grid);
 hipError_t launch_peak_mfma(hipStream_t st, float* sink, int grid, int iters);
 
+// ---- kernels of the caches that hold 4-bit rows, and of the head's scores
+// (cache_kernels.h, score_kernels.h)
+
+enum KvKind { KV_F32 = 0, KV_BF16 = 1, KV_INT4 = 2 };
+// Elements are bytes here: a cell is 16 positions of one KV head, K and V.
+__host__ __device__ constexpr size_t kv_cell_bytes(int kind, int hd) {
+  return kind == KV_INT4 ? (size_t)16 * hd + 128 : (size_t)2 * kBlock * hd * (kind == KV_BF16 ? 2 : 4);
+}
+// Where a row's position lies: block tables[key[row] * mul + pos / 16], with
+// key in [0, n_keys), pos / 16 < table_len and block < num_blocks.
+struct KvPlace { const int *tables, *key; int mul, n_keys, table_len, num_blocks; };
+
+struct AppendArgs {
+  const void* x;           // rows of (n_h + 2 n_kv) * hd, `stride` elements apart
+  size_t stride;
+  int nsplit;              // f32 rows: partial sums to add, split_stride apart (1: none)
+  size_t split_stride;
+  const int* row_pos;
+  KvPlace place;
+  const float2* rope;      // [rope_len][hd / 2], or null
+  int rope_len;
+  ModelPtrs q_gain, k_gain;// per model, [hd]; entry 0 null: no norm
+  const int* row_model;    // null: model 0
+  bool gain_bf16;
+  float eps;
+  void* q;                 // [T][n_h][hd]
+  void* kv;
+  int layer, n_h, n_kv, hd, T;
+};
+// x_bf16: rows and q are bf16 (else f32).
+hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a);
+hipError_t launch_kv_read(hipStream_t st, int kind, const void* kv, int layer, int n_kv, int hd, int T,
+                          const int* row_pos, const KvPlace& place, void* k, void* v);
+
+// Attention over 4-bit cells. Types of q and out: f32, bf16, or (out only) the
+// split-bf16 pair of the GEMM inputs, lo plane out_lo elements after hi.
+enum OutType { OUT_F32 = 0, OUT_BF16 = 1, OUT_SPLIT = 2 };
+struct Attend4Args {
+  const void* q;
+  size_t q_stride;
+  bool q_bf16;
+  void* out;               // [T][n_h][hd]
+  size_t out_lo;
+  int out_type;
+  const void* kv;
+  int layer, num_blocks, n_h, n_kv, hd;
+  float scale;
+  const int* tables;       // block ids
+  // rows: row r sees min(row_ctx[r], max_ctx) keys of table row row_seq[r]
+  const int *row_seq, *row_ctx;
+  // chunks: rows [start[i], start[i + 1]) end at position ctx[i] - 1 of table row i
+  const int *chunk_start, *chunk_ctx;
+  int T, n_seqs, table_len, max_ctx;
+};
+hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace);
+hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* workspace);
+size_t attend4_rows_bytes(int n_h, int hd, int T, int max_ctx);
+size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx);
+
+constexpr int kMaxTop = 32;
+struct ScoreArgs {
+  const void* logits;
+  bool bf16;
+  size_t stride;
+  int rows, vocab, top;
+  const int* tokens;
+  float *logprob, *entropy;
+  int* top_ids;
+  float* top_logprobs;
+};
+hipError_t launch_score(hipStream_t st, const ScoreArgs& a, void* workspace);
+size_t score_bytes(int rows, int vocab, int top);
+
 }  // namespace moa

@@ -2261,4 +2261,7 @@ hipError_t launch_argmax(hipStream_t st, const float* logits, int R, int V, cons
   return hipGetLastError();
 }
 
+#include "cache_kernels.h"
+#include "score_kernels.h"
+
 }  // namespace moa

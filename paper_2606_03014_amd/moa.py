@@ -14,6 +14,8 @@ MOA_OK, MOA_EINVAL, MOA_ENOMEM, MOA_ENOSPC, MOA_ESTATE, MOA_EHIP = 0, -1, -2, -3
 MOA_F32, MOA_BF16 = 0, 1
 MOA_FLAG_PLAN_ONLY = 1
 MOA_FLAG_ONE_STREAM = 2
+MOA_KV_F32, MOA_KV_BF16, MOA_KV_INT4 = 0, 1, 2
+MOA_MAX_TOP = 32
 STATUS_NAMES = {0: "MOA_OK", -1: "MOA_EINVAL", -2: "MOA_ENOMEM", -3: "MOA_ENOSPC",
                 -4: "MOA_ESTATE", -5: "MOA_EHIP"}
 
@@ -55,6 +57,11 @@ class moa_kernel_stats(C.Structure):
                 ("roof_ms_all", C.c_double)]
 
 
+class moa_kv_cfg(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("n_layers", C.c_int32), ("num_blocks", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
 KERNEL_CLASSES = ["embed", "norm", "gemm_qkv", "rope_kv", "attn", "attn_reduce", "gemm_o",
                   "gemm_gateup", "gemm_down", "gemm_lmhead", "argmax", "prefill_attn",
                   "gemm_small_m", "gemm_large_m"]
@@ -62,6 +69,7 @@ KERNEL_CLASSES = ["embed", "norm", "gemm_qkv", "rope_kv", "attn", "attn_reduce",
 VIEW_CLASSES = ("gemm_small_m", "gemm_large_m")
 
 P = C.POINTER
+_D, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 _SIGS = {
     "moa_arena_bytes": (C.c_int, [P(moa_engine_cfg), P(C.c_size_t)]),
     "moa_create": (C.c_int, [P(moa_engine_cfg), C.c_void_p, C.c_size_t, C.c_void_p, P(C.c_void_p)]),
@@ -86,6 +94,19 @@ _SIGS = {
     "moa_debug_measure_peaks": (C.c_int, [C.c_void_p, P(C.c_double), P(C.c_double)]),
     "moa_debug_step_shares": (C.c_int, [C.c_void_p, P(C.c_int32), P(C.c_int32), P(C.c_int32), P(C.c_double),
                                         P(C.c_int32), P(C.c_int32), P(C.c_int32)]),
+    # operators: device pointers as integers (see ops.py)
+    "moa_kv_bytes": (C.c_int, [P(moa_kv_cfg), P(C.c_size_t)]),
+    "moa_kv_append": (C.c_int, [P(moa_kv_cfg), _D, _I, _D, _I, _L, _I, _D, _D, _D, _I, _I, _D, _I, _D, _D, _I,
+                                C.c_float, _D, _D]),
+    "moa_kv_read": (C.c_int, [P(moa_kv_cfg), _D, _I, _I, _D, _D, _D, _I, _I, _D, _D, _D]),
+    "moa_kv_attend_bytes": (C.c_int, [P(moa_kv_cfg), _I, _I, P(C.c_size_t)]),
+    "moa_kv_attend": (C.c_int, [P(moa_kv_cfg), _D, _I, _D, _I, _L, _I, _D, _D, _D, _I, _I, _I, C.c_float, _D, _D,
+                                C.c_size_t, _D]),
+    "moa_kv_attend_chunks_bytes": (C.c_int, [P(moa_kv_cfg), _I, _I, _I, P(C.c_size_t)]),
+    "moa_kv_attend_chunks": (C.c_int, [P(moa_kv_cfg), _D, _I, _D, _I, _L, _I, _D, _D, _D, _I, _I, _I, C.c_float, _D,
+                                       _D, C.c_size_t, _D]),
+    "moa_score_tokens_bytes": (C.c_int, [_I, _I, _I, P(C.c_size_t)]),
+    "moa_score_tokens": (C.c_int, [_D, _I, _L, _I, _I, _D, _D, _D, _I, _D, _D, _D, C.c_size_t, _D]),
 }
 
 _lib = None
