@@ -304,6 +304,373 @@ __global__ __launch_bounds__(64) void k_attend4(Attend4Args a) {
   }
 }
 
+// ---------------------------- decode attention over 4-bit cells (16x16x32 MFMA)
+// One workgroup is a row, a KV head and up to kSplit4 of its keys; its four waves take
+// every fourth tile of 64 keys (four blocks) and join at the end.
+//
+// A code reaches the matrix cores as it is: its four bits, moved to bits 4 to 7 of a
+// half, are the float16 2^-20 c (subnormal, and exact), so seven integer instructions
+// unpack eight codes, and scales and minima are applied after the products, per key:
+//   q . k = s_k sum(c q) + m_k sum(q),   sum p v = sum (p s_v) c + sum p m_v.
+// q, scaled to a power of two below 2^13, and p s_v enter as pairs of float16 (hi + lo, 22
+// bits): the head's hi part is column h of an operand and its lo part column h + 8, so
+// the pair costs no product. The code bits lie as high in the half as a mask without
+// a shift for one pair in four allows: at bits 0 to 3 the products lose four more bits
+// in the matrix cores (3.6e-6 of the sum against 6.8e-8, measured).
+//
+// S^T = K Q^T: row r of score tile n is block r / 4, slot 4 n + r % 4 of the 64 keys, so a
+// lane (col, q = lane / 16) ends with the scores of slots 0 to 15 of block q, which are
+// the k-slots that O^T = V^T P^T wants from it: no probability crosses lanes. V's cells
+// are laid out for that product (16 slots of a dim side by side): nothing is transposed.
+//
+// The softmax's reference M is kept so that p s_v stays below 2^13 (float16 holds it) and is
+// moved, with everything that was summed, only when a product passes that; p alone
+// may be as large as 2^98 then (tiny scales), which float32 sums hold.
+#ifndef A4_SPLIT
+#define A4_SPLIT 1024
+#endif
+constexpr int kSplit4 = A4_SPLIT;
+constexpr unsigned kCodeMask = 0x00F000F0u;
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+
+struct Partial4 { float *acc, *ml; };              // [slot][n_h][hd] sums; [slot][n_h] (M, l)
+
+// (a, b) -> two float16 in one word, round to nearest even: a truncated lo part would
+// put a bias of 2^-23 on every probability, and the codes, which are all positive, and
+// the minima nearly cancel in the answer (6e-6 of it over 900 equal probabilities).
+__device__ __forceinline__ unsigned pack_f16(float a, float b) {
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
+}
+// Over a column of four lanes 16 apart.
+__device__ __forceinline__ float max_column(float v) {
+  v = fmaxf(v, swz_xor16(v));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_column(float v) {
+  v += swz_xor16(v);
+  return v + __shfl_xor(v, 32, 64);
+}
+// Two codes, at bits 0 to 3 of each half after the shift, as float16 c - 8.
+__device__ __forceinline__ unsigned centred(unsigned w) {
+  const f16x2_t x = __builtin_bit_cast(f16x2_t, (w & 0x03C003C0u) | 0x4C004C00u);   // 16 + c
+  return __builtin_bit_cast(unsigned, x - (f16x2_t){(_Float16)24, (_Float16)24});
+}
+// Eight codes of a word as float16 2^-20 c, in the order 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ u32x4 codes_f16(unsigned w) {
+  return u32x4{(w << 4) & kCodeMask, w & kCodeMask, (w >> 4) & kCodeMask, (w >> 8) & kCodeMask};
+}
+
+// n consecutive elements as float32; vec: 16-byte loads may be used.
+template <int N>
+__device__ __forceinline__ void load_run(const void* p, size_t at, bool bf16, bool vec, float* v) {
+  if (vec && bf16) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      const u32x4 x = *(const u32x4*)((const uint16_t*)p + at + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[i + 2 * k] = __uint_as_float(x[k] << 16);
+        v[i + 2 * k + 1] = __uint_as_float(x[k] & 0xffff0000u);
+      }
+    }
+  } else if (vec) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const f32x4_t x = *(const f32x4_t*)((const float*)p + at + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[i + k] = x[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = bf16 ? load_el<true>(p, at + i) : load_el<false>(p, at + i);
+  }
+}
+
+#ifndef A4_WPE
+#define A4_WPE 2
+#endif
+template <int HD, bool ITEMS, bool FINE>
+__global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, const AttnItem* __restrict__ items, Partial4 part,
+                                                         bool q_vec) {
+  constexpr int CELL = (int)kv_cell_bytes(KV_INT4, HD);
+  constexpr int W = HD / 32;                       // words of a key's row per lane; 16-dim tiles of half a head
+  __shared__ __align__(16) float ssc[4][2][4][36]; // wave: K and V (s, m) of 4 blocks of 16 keys, blocks 36 words apart
+  __shared__ float sml[4][2][8];
+  __shared__ __align__(16) float so[4][8][HD];
+  __shared__ unsigned sid[kSplit4 / kBlock];       // the split's blocks
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4, gq = a.n_h / a.n_kv, kvh = blockIdx.x % a.n_kv;
+  const int item = blockIdx.x / a.n_kv;            // heads fastest, then rows: every XCD gets its part of each split
+  int row, k0, k1, slot;
+  const int* tab;
+  if constexpr (ITEMS) {
+    const AttnItem it = items[item];
+    row = it.row; k0 = it.k0; k1 = it.k1; slot = it.slot;
+    tab = a.tables + it.bt_off - (it.k0 >> 4);
+  } else {
+    row = item % a.T;
+    const int sp = item / a.T;
+    const int seq = a.row_seq[row];
+    const int ctx = (unsigned)seq < (unsigned)a.n_seqs ? min(a.row_ctx[row], a.max_ctx) : 0;
+    k0 = sp * kSplit4;
+    k1 = min(ctx, k0 + kSplit4);
+    slot = ctx > kSplit4 ? item : -1;
+    tab = a.tables + (size_t)max(seq, 0) * a.table_len;
+    if (k0 >= k1) {
+      if (sp > 0 || ctx > 0) return;
+      for (int i = threadIdx.x; i < gq * HD; i += 256) {     // a row without keys
+        const size_t o = ((size_t)row * a.n_h + kvh * gq) * HD + i;
+        if (a.out_type == OUT_F32) ((float*)a.out)[o] = 0.f;
+        else ((uint16_t*)a.out)[o] = 0;
+      }
+      return;
+    }
+  }
+  const unsigned char* pool = (const unsigned char*)a.kv + ((size_t)a.layer * a.num_blocks * a.n_kv + kvh) * CELL;
+  const size_t stride = (size_t)a.n_kv * CELL;
+  // Block ids lie in LDS: an address then never waits for a global load, which (vector
+  // loads complete in order) would wait for every tile in flight too. Behind the last
+  // key they repeat the last block.
+  {
+    const int b0 = k0 >> 4, last = (k1 - 1) >> 4;
+    for (int i = threadIdx.x; i < kSplit4 / kBlock; i += 256)
+      sid[i] = min((unsigned)tab[min(b0 + i, last)], (unsigned)a.num_blocks - 1u);
+  }
+
+  // B operand of the scores: lane (col, quad) holds head col % 8's part col / 8 of dims 8 (W quad + j) .. + 8
+  u32x4 qf[W];
+  float Q, f;                                      // sum of the head's q; a score's unit in powers of two
+  {
+    const int h = col & 7;
+    float v[W][8], mx = 0.f;
+    const size_t qo = (size_t)row * a.q_stride + (size_t)(kvh * gq + min(h, gq - 1)) * HD + 8 * W * quad;
+    const float sc = h < gq ? a.scale * 1.4426950408889634f : 0.f;
+    load_run<8 * W>(a.q, qo, a.q_bf16, q_vec, &v[0][0]);
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        o[i] = v[j][(i >> 1) + (i & 1) * 4] * sc;            // the order of codes_f16
+        mx = fmaxf(mx, fabsf(o[i]));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = o[i];
+    }
+    mx = max_column(mx);
+    int e = 0;
+    if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
+    f = ldexpf(1.f, e - 13);
+    const float up = ldexpf(1.f, 13 - e);
+    const unsigned lo = col >= 8 ? 0xffffffffu : 0u;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = v[j][2 * i] * up, y = v[j][2 * i + 1] * up;
+        const f16x2_t hi = __builtin_bit_cast(f16x2_t, pack_f16(x, y) & lo);
+        qf[j][i] = pack_f16(x - (float)hi[0], y - (float)hi[1]);
+        const f16x2_t g = __builtin_bit_cast(f16x2_t, (unsigned)qf[j][i]);
+        sum += (float)g[0] + (float)g[1];
+      }
+    sum = sum_column(sum);
+    Q = sum + dpp<0x128>(sum);
+  }
+  const unsigned lomask = col >= 8 ? 0xffffffffu : 0u;
+
+  f32x4_t acc[2 * W];
+#pragma unroll
+  for (int i = 0; i < 2 * W; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float M = -INFINITY, l = 0.f, mv = 0.f;
+  const int b0 = k0 >> 4;
+  auto block = [&](int b) { return sid[min(b - b0, kSplit4 / kBlock - 1)]; };
+  __syncthreads();
+  struct Tile { unsigned kw[4][W]; u32x4 vw[W]; unsigned ks, vs; };
+  auto load = [&](int t, Tile& x) {
+    const unsigned char* kp = pool + block(4 * t + (col >> 2)) * stride + (lane & 3) * (HD / 2) + quad * (HD / 8);
+    const unsigned char* vp = pool + block(4 * t + quad) * stride + 8 * HD + col * 16;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      if constexpr (W == 4) {
+        const u32x4 y = *(const u32x4*)(kp + n * 2 * HD);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.kw[n][j] = y[j];
+      } else {
+        const u32x2_t y = *(const u32x2_t*)(kp + n * 2 * HD);
+        x.kw[n][0] = y[0]; x.kw[n][1] = y[1];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) x.vw[i] = *(const u32x4*)(vp + i * 256);
+    // this lane's key: slot col of block quad
+    x.ks = *(const unsigned*)(vp + 8 * HD - col * 12);
+    x.vs = *(const unsigned*)(vp + 8 * HD + 64 - col * 12);
+  };
+#if 1
+  Tile nxt;
+  load((k0 >> 6) + w, nxt);
+#endif
+  for (int t = (k0 >> 6) + w; t * 64 < k1; t += 4) {
+#if 1
+    const Tile cur = nxt;
+    load(t + 4, nxt);
+#else
+    Tile cur;
+    load(t, cur);
+#endif
+    const auto& kw = cur.kw;
+    const auto& vw = cur.vw;
+    unsigned ks = cur.ks, vs = cur.vs;
+    if (64 * t + lane >= k1) ks = vs = 0;          // whatever lies behind the last key
+    *(float2*)&ssc[w][0][quad][2 * col] = make_float2(__uint_as_float(ks << 16) * 1048576.f, __uint_as_float(ks & 0xffff0000u));
+    *(float2*)&ssc[w][1][quad][2 * col] = make_float2(__uint_as_float(vs << 16), fmaf(__uint_as_float(vs << 16), FINE ? 8.f : 0.f, __uint_as_float(vs & 0xffff0000u)));
+    wave_lds_fence();
+
+    float s[16];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      f32x4_t d = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, codes_f16(kw[n][j])),
+                                                   __builtin_bit_cast(f16x8_t, qf[j]), d, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 sm = *(const float2*)&ssc[w][0][quad][2 * (4 * n + i)];
+        s[4 * n + i] = fmaf(sm.x, d[i] + dpp<0x128>(d[i]), sm.y * Q);
+      }
+    }
+    if (64 * t + 64 > k1) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (64 * t + 16 * quad + e >= k1) s[e] = -INFINITY;
+    }
+    float pv[16], sv[16], ts, tm, pm;
+    auto probabilities = [&] {
+      ts = tm = pm = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[e], f, -M));
+        const float2 sm = *(const float2*)&ssc[w][1][quad][2 * e];
+        sv[e] = sm.x;
+        pv[e] = p * sm.x;
+        ts += p;
+        tm = fmaf(p, sm.y, tm);
+        pm = fmaxf(pm, pv[e]);
+      }
+    };
+    const bool first = __any(M == -INFINITY);
+    if (!first) probabilities();
+    if (first || !__all(pm <= 8192.f && ts < INFINITY)) {
+      float u = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float2 sm = *(const float2*)&ssc[w][1][quad][2 * e];
+        u = fmaxf(u, fmaf(s[e], f, fmaxf(__builtin_amdgcn_logf(sm.x), -90.f)));
+      }
+      u = fmaxf(max_column(u) - 8.f, M);
+      const float alpha = __builtin_amdgcn_exp2f(M - u);
+      M = u;
+      l *= alpha;
+      mv *= alpha;
+#pragma unroll
+      for (int i = 0; i < 2 * W; ++i) acc[i] *= alpha;
+      probabilities();
+    }
+    l += ts;
+    mv += tm;
+    // P^T: k-slots 0 to 7 of step h are slots 8 h + 0 2 1 3 4 6 5 7 of block quad
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 pf;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = 8 * h + 4 * (i >> 1) + (i & 1);
+        const f16x2_t hi = __builtin_bit_cast(f16x2_t, pack_f16(pv[e], pv[e + 2]) & lomask);
+        pf[i] = pack_f16(pv[e] - (float)hi[0], pv[e + 2] - (float)hi[1]);
+      }
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const unsigned x = vw[i][2 * h], y = vw[i][2 * h + 1];
+        u32x4 lo, hi;
+        if constexpr (FINE) {
+          lo = u32x4{centred(x << 6), centred(x >> 2), centred(y << 6), centred(y >> 2)};
+          hi = u32x4{centred(x << 2), centred(x >> 6), centred(y << 2), centred(y >> 6)};
+        } else {
+          lo = u32x4{(x << 4) & kCodeMask, (x >> 4) & kCodeMask, (y << 4) & kCodeMask, (y >> 4) & kCodeMask};
+          hi = u32x4{x & kCodeMask, (x >> 8) & kCodeMask, y & kCodeMask, (y >> 8) & kCodeMask};
+        }
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, lo), __builtin_bit_cast(f16x8_t, pf), acc[i], 0, 0, 0);
+        acc[W + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, hi), __builtin_bit_cast(f16x8_t, pf), acc[W + i], 0, 0, 0);
+      }
+    }
+    wave_lds_fence();
+  }
+
+  // join the lanes of a head, then the waves
+  l = sum_column(l);
+  mv = sum_column(mv);
+  if (quad == 0 && col < 8) { sml[w][0][col] = M; sml[w][1][col] = l; }
+#pragma unroll
+  for (int i = 0; i < 2 * W; ++i) {
+    f32x4_t o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = fmaf(acc[i][k] + dpp<0x128>(acc[i][k]), FINE ? 1.f : 1048576.f, mv);
+    if (col < gq) *(f32x4_t*)&so[w][col][16 * i + 4 * quad] = o;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < gq * HD; i += 256) {
+    const int h = i / HD, d = i % HD;
+    float Mt = sml[0][0][h];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) Mt = fmaxf(Mt, sml[k][0][h]);
+    float lt = 0.f, ot = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float x = __builtin_amdgcn_exp2f(sml[k][0][h] - Mt);       // a wave without keys: 0
+      lt = fmaf(sml[k][1][h], x, lt);
+      ot = fmaf(so[k][h][d], x, ot);
+    }
+    const int head = kvh * gq + h;
+    if (slot >= 0) {
+      const size_t o = (size_t)slot * a.n_h + head;
+      part.acc[o * HD + d] = ot;
+      if (d == 0) { part.ml[2 * o] = Mt; part.ml[2 * o + 1] = lt; }
+    } else {
+      const size_t o = ((size_t)row * a.n_h + head) * HD + d;
+      const float r = ot / lt;
+      if (a.out_type == OUT_F32) ((float*)a.out)[o] = r;
+      else if (a.out_type == OUT_BF16) ((uint16_t*)a.out)[o] = f2bf(r);
+      else store_split((uint16_t*)a.out, a.out_lo, o, r);
+    }
+  }
+}
+
+// The join of a row's splits, in their order.
+template <int HD>
+__global__ __launch_bounds__(HD) void k_attend4_join(Attend4Args a, Partial4 part) {
+  const int row = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+  const int seq = a.row_seq[row];
+  const int ctx = (unsigned)seq < (unsigned)a.n_seqs ? min(a.row_ctx[row], a.max_ctx) : 0;
+  if (ctx <= kSplit4) return;
+  const int n = (ctx + kSplit4 - 1) / kSplit4;
+  float M = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const size_t b = ((size_t)s * a.T + row) * a.n_h + h;
+    const float ms = part.ml[2 * b], ls = part.ml[2 * b + 1], as = part.acc[b * HD + d];
+    const float mn = fmaxf(M, ms), x = __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(ms - mn);
+    l = l * x + ls * y;
+    o = o * x + as * y;
+    M = mn;
+  }
+  const size_t at = ((size_t)row * a.n_h + h) * HD + d;
+  if (a.out_type == OUT_F32) ((float*)a.out)[at] = o / l;
+  else ((uint16_t*)a.out)[at] = f2bf(o / l);
+}
+
 // =============================================================== launchers
 
 hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a) {
@@ -342,8 +709,31 @@ hipError_t launch_kv_read(hipStream_t st, int kind, const void* kv, int layer, i
   return hipGetLastError();
 }
 
-size_t attend4_rows_bytes(int, int, int, int) { return 0; }
+static int splits4(int max_ctx) { return (max_ctx + kSplit4 - 1) / kSplit4; }
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+size_t attend4_rows_bytes(int n_h, int hd, int T, int max_ctx) {
+  const size_t slots = splits4(max_ctx) > 1 ? (size_t)T * splits4(max_ctx) : 0;
+  return up256(slots * n_h * hd * 4) + slots * n_h * 8;
+}
 size_t attend4_chunks_bytes(int, int, int, int, int, int) { return 0; }
+
+hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace) {
+  if (a.T <= 0) return hipSuccess;
+  const int n = splits4(a.max_ctx);
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)a.T * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
+  Partial4 part{(float*)workspace, (float*)((char*)workspace + up256((size_t)a.T * n * a.n_h * a.hd * 4))};
+  const dim3 grid((unsigned)(a.T * n * a.n_kv)), blk(256);
+  const bool vec = a.q_stride % (a.q_bf16 ? 8 : 4) == 0 && (uintptr_t)a.q % 16 == 0;
+  auto go = [&](auto kern) { klaunch(kern, grid, blk, st, a, (const AttnItem*)nullptr, part, vec); };
+  if (a.hd == 64) a.q_bf16 ? go(k_attend4_rows<64, false, false>) : go(k_attend4_rows<64, false, true>);
+  else a.q_bf16 ? go(k_attend4_rows<128, false, false>) : go(k_attend4_rows<128, false, true>);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || n == 1) return err;
+  if (a.hd == 64) klaunch(k_attend4_join<64>, dim3(a.T, a.n_h), dim3(64), st, a, part);
+  else klaunch(k_attend4_join<128>, dim3(a.T, a.n_h), dim3(128), st, a, part);
+  return hipGetLastError();
+}
 
 static hipError_t attend4(hipStream_t st, const Attend4Args& a) {
   if (a.T <= 0) return hipSuccess;
@@ -353,5 +743,4 @@ static hipError_t attend4(hipStream_t st, const Attend4Args& a) {
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
-hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void*) { return attend4(st, a); }
 hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void*) { return attend4(st, a); }
