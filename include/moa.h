@@ -409,13 +409,15 @@ moa_status moa_kv_read(const moa_kv_cfg* cfg, const void* kv, int32_t layer, int
 /* Attention of decode rows over a 4-bit pool: row r's query heads see keys
  * [0, c), c = min(row_ctx[r], max_ctx), of sequence row_seq[r], and out[r]
  * [n_heads][D] = softmax(scale * q . k) . v. q rows (n_heads * D elements) and
- * out are of `type`; sums, the softmax and its statistics are float32, q and
- * the probabilities enter the products with at least 16 significant bits. A
+ * out are of `type`; sums, the softmax and its statistics are float32. q and
+ * the probabilities enter the products with 22 significant bits in float32
+ * calls; in bf16 ones q is exact and the probabilities have 11. A
  * row with c <= 0 or a sequence out of range is 0 (rows of one call may share
  * a sequence and may see fewer keys than it has). max_ctx bounds the work
  * (1 <= max_ctx <= 16 table_len): the keys of long rows are split among
- * workgroups and joined in a fixed order, in splits that depend on nothing
- * but the row. Block ids out of range are read as the pool's last block.
+ * workgroups and joined in a fixed order, in splits that depend on n_rows,
+ * n_kv_heads and max_ctx alone; between those the bits of a row hang on
+ * nothing but the row. Block ids out of range are read as the pool's last block.
  * EINVAL too: the pool is not INT4. */
 moa_status moa_kv_attend_bytes(const moa_kv_cfg* cfg, int32_t n_rows, int32_t max_ctx, size_t* bytes);
 moa_status moa_kv_attend(const moa_kv_cfg* cfg, const void* kv, int32_t layer, const void* q, int32_t type,

@@ -305,7 +305,7 @@ __global__ __launch_bounds__(64) void k_attend4(Attend4Args a) {
 }
 
 // ---------------------------- decode attention over 4-bit cells (16x16x32 MFMA)
-// One workgroup is a row, a KV head and up to kSplit4 of its keys; its four waves take
+// One workgroup is a row, a KV head and one split of its keys; its four waves take
 // every fourth tile of 64 keys (four blocks) and join at the end.
 //
 // A code reaches the matrix cores as it is: its four bits, moved to bits 4 to 7 of a
@@ -326,10 +326,7 @@ __global__ __launch_bounds__(64) void k_attend4(Attend4Args a) {
 // The softmax's reference M is kept so that p s_v stays below 2^13 (float16 holds it) and is
 // moved, with everything that was summed, only when a product passes that; p alone
 // may be as large as 2^98 then (tiny scales), which float32 sums hold.
-#ifndef A4_SPLIT
-#define A4_SPLIT 1024
-#endif
-constexpr int kSplit4 = A4_SPLIT;
+constexpr int kSplit4Max = 2048;
 constexpr unsigned kCodeMask = 0x00F000F0u;
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
@@ -356,7 +353,12 @@ __device__ __forceinline__ unsigned centred(unsigned w) {
   const f16x2_t x = __builtin_bit_cast(f16x2_t, (w & 0x03C003C0u) | 0x4C004C00u);   // 16 + c
   return __builtin_bit_cast(unsigned, x - (f16x2_t){(_Float16)24, (_Float16)24});
 }
-// Eight codes of a word as float16 2^-20 c, in the order 0 4 1 5 2 6 3 7.
+// Eight codes of a word as float16, in the order 0 4 1 5 2 6 3 7: 2^-20 c; or 2^-24 c and,
+// for odd ones, 2^-20 c (two instructions fewer).
+__device__ __forceinline__ u32x4 codes_mixed(unsigned w) {
+  const unsigned v = w >> 8;
+  return u32x4{w & 0x000F000Fu, w & kCodeMask, v & 0x000F000Fu, v & kCodeMask};
+}
 __device__ __forceinline__ u32x4 codes_f16(unsigned w) {
   return u32x4{(w << 4) & kCodeMask, w & kCodeMask, (w >> 4) & kCodeMask, (w >> 8) & kCodeMask};
 }
@@ -387,174 +389,168 @@ __device__ __forceinline__ void load_run(const void* p, size_t at, bool bf16, bo
   }
 }
 
-#ifndef A4_WPE
-#define A4_WPE 2
-#endif
 template <int HD, bool ITEMS, bool FINE>
-__global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, const AttnItem* __restrict__ items, Partial4 part,
-                                                         bool q_vec) {
+__global__ __launch_bounds__(256, 3) void k_attend4_rows(Attend4Args a, const AttnItem* __restrict__ items, int split,
+                                                         Partial4 part, bool q_vec) {
   constexpr int CELL = (int)kv_cell_bytes(KV_INT4, HD);
   constexpr int W = HD / 32;                       // words of a key's row per lane; 16-dim tiles of half a head
   __shared__ __align__(16) float ssc[4][2][4][36]; // wave: K and V (s, m) of 4 blocks of 16 keys, blocks 36 words apart
   __shared__ float sml[4][2][8];
-  __shared__ __align__(16) float so[4][8][HD];
-  __shared__ unsigned sid[kSplit4 / kBlock];       // the split's blocks
+  __shared__ __align__(16) float so[4][8][HD + 4];
+  __shared__ unsigned sid[kSplit4Max / kBlock];       // the split's blocks
+  __shared__ __align__(16) unsigned sq[W][69][4];  // the queries' fragments (lane + lane / 16: other banks)
+  __shared__ float sqf[2][8];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4, gq = a.n_h / a.n_kv, kvh = blockIdx.x % a.n_kv;
   const int item = blockIdx.x / a.n_kv;            // heads fastest, then rows: every XCD gets its part of each split
-  int row, k0, k1, slot;
+  int row, k0, k1, slot, last;                     // last: the last table entry that may be read
   const int* tab;
   if constexpr (ITEMS) {
     const AttnItem it = items[item];
     row = it.row; k0 = it.k0; k1 = it.k1; slot = it.slot;
     tab = a.tables + it.bt_off - (it.k0 >> 4);
+    last = (k1 - 1) >> 4;
   } else {
     row = item % a.T;
-    const int sp = item / a.T;
+    k0 = item / a.T * split;
     const int seq = a.row_seq[row];
-    const int ctx = (unsigned)seq < (unsigned)a.n_seqs ? min(a.row_ctx[row], a.max_ctx) : 0;
-    k0 = sp * kSplit4;
-    k1 = min(ctx, k0 + kSplit4);
-    slot = ctx > kSplit4 ? item : -1;
-    tab = a.tables + (size_t)max(seq, 0) * a.table_len;
-    if (k0 >= k1) {
-      if (sp > 0 || ctx > 0) return;
-      for (int i = threadIdx.x; i < gq * HD; i += 256) {     // a row without keys
-        const size_t o = ((size_t)row * a.n_h + kvh * gq) * HD + i;
-        if (a.out_type == OUT_F32) ((float*)a.out)[o] = 0.f;
-        else ((uint16_t*)a.out)[o] = 0;
-      }
-      return;
+    const bool known = (unsigned)seq < (unsigned)a.n_seqs;
+    tab = a.tables + (known ? (size_t)seq * a.table_len : 0);
+    last = a.table_len - 1;
+    const int ctx = known ? min(a.row_ctx[row], a.max_ctx) : 0;
+    k1 = min(ctx, k0 + split);
+    slot = ctx > split ? item : -1;
+  }
+  const int t0 = (k0 >> 6) + w, b0 = k0 >> 4;
+  // Block ids lie in LDS, those of the first tile beside them in registers: an address
+  // then never waits for a global load, which (vector loads complete in order) would
+  // wait for every tile in flight too; and no id waits for the context's length.
+  auto id_of = [&](int b) { return min((unsigned)tab[min(b, last)], (unsigned)a.num_blocks - 1u); };
+  const unsigned kid = id_of(4 * t0 + (col >> 2)), vid = id_of(4 * t0 + quad);
+  for (int i = threadIdx.x; i < split / kBlock; i += 256) sid[i] = id_of(b0 + i);
+  if (!ITEMS && k0 >= k1) {
+    if (k0 > 0) return;
+    for (int i = threadIdx.x; i < gq * HD; i += 256) {       // a row without keys
+      const size_t o = ((size_t)row * a.n_h + kvh * gq) * HD + i;
+      if (a.out_type == OUT_F32) ((float*)a.out)[o] = 0.f;
+      else ((uint16_t*)a.out)[o] = 0;
     }
+    return;
   }
   const unsigned char* pool = (const unsigned char*)a.kv + ((size_t)a.layer * a.num_blocks * a.n_kv + kvh) * CELL;
   const size_t stride = (size_t)a.n_kv * CELL;
-  // Block ids lie in LDS: an address then never waits for a global load, which (vector
-  // loads complete in order) would wait for every tile in flight too. Behind the last
-  // key they repeat the last block.
-  {
-    const int b0 = k0 >> 4, last = (k1 - 1) >> 4;
-    for (int i = threadIdx.x; i < kSplit4 / kBlock; i += 256)
-      sid[i] = min((unsigned)tab[min(b0 + i, last)], (unsigned)a.num_blocks - 1u);
-  }
-
-  // B operand of the scores: lane (col, quad) holds head col % 8's part col / 8 of dims 8 (W quad + j) .. + 8
-  u32x4 qf[W];
-  float Q, f;                                      // sum of the head's q; a score's unit in powers of two
-  {
-    const int h = col & 7;
-    float v[W][8], mx = 0.f;
-    const size_t qo = (size_t)row * a.q_stride + (size_t)(kvh * gq + min(h, gq - 1)) * HD + 8 * W * quad;
-    const float sc = h < gq ? a.scale * 1.4426950408889634f : 0.f;
-    load_run<8 * W>(a.q, qo, a.q_bf16, q_vec, &v[0][0]);
+  // A tile's keys (and scales) and values are reloaded for the next tile as soon as they are
+  // used: keys while the softmax and P V run, values while the next scores do.
+  unsigned kw[4][W], ks, vs;
+  u32x4 vw[W];
+  auto load_k = [&](unsigned kb, unsigned vb) {
+    const unsigned char* kp = pool + kb * stride + (lane & 3) * (HD / 2) + quad * (HD / 8);
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      float o[8];
+    for (int n = 0; n < 4; ++n) {
+      if constexpr (W == 4) {
+        const u32x4 y = __builtin_nontemporal_load((const u32x4*)(kp + n * 2 * HD));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        o[i] = v[j][(i >> 1) + (i & 1) * 4] * sc;            // the order of codes_f16
-        mx = fmaxf(mx, fabsf(o[i]));
+        for (int j = 0; j < 4; ++j) kw[n][j] = y[j];
+      } else {
+        const u32x2_t y = __builtin_nontemporal_load((const u32x2_t*)(kp + n * 2 * HD));
+        kw[n][0] = y[0]; kw[n][1] = y[1];
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = o[i];
     }
-    mx = max_column(mx);
-    int e = 0;
-    if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
-    f = ldexpf(1.f, e - 13);
-    const float up = ldexpf(1.f, 13 - e);
-    const unsigned lo = col >= 8 ? 0xffffffffu : 0u;
-    float sum = 0.f;
+    // this lane's key: slot col of block quad
+    const unsigned* sp = (const unsigned*)(pool + vb * stride + 16 * HD) + col;
+    ks = __builtin_nontemporal_load(sp);
+    vs = __builtin_nontemporal_load(sp + 16);
+  };
+  auto load_v = [&](unsigned vb) {
+    const unsigned char* vp = pool + vb * stride + 8 * HD + col * 16;
 #pragma unroll
-    for (int j = 0; j < W; ++j)
+    for (int i = 0; i < W; ++i) vw[i] = __builtin_nontemporal_load((const u32x4*)(vp + i * 256));
+  };
+  load_k(kid, vid);
+  load_v(vid);
+
+  // B operand of the scores, made once by all threads: lane (col, quad) of step j holds head
+  // col % 8's part col / 8 of dims 8 (W quad + j) .. + 8, in the order of the codes.
+  {
+    constexpr int TH = HD / 4;                     // threads a head: four dims each
+    const int h = threadIdx.x / TH, d = (threadIdx.x % TH) * 4;
+    if (h < 8) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (h < gq) load_run<4>(a.q, (size_t)row * a.q_stride + (size_t)(kvh * gq + h) * HD + d, a.q_bf16, q_vec, v);
+      float mx = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+      mx = max16(mx);
+      if constexpr (TH == 32) mx = fmaxf(mx, swz_xor16(mx));
+      int e = 0;
+      if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
+      const float up = a.scale > 0.f ? ldexpf(1.f, 13 - e) : (a.scale < 0.f ? -ldexpf(1.f, 13 - e) : 0.f);
+      float sum = 0.f;
+      uint16_t* hi = (uint16_t*)sq[(d >> 3) % W][17 * ((d >> 3) / W) + h] + ((d >> 2) & 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = v[j][2 * i] * up, y = v[j][2 * i + 1] * up;
-        const f16x2_t hi = __builtin_bit_cast(f16x2_t, pack_f16(x, y) & lo);
-        qf[j][i] = pack_f16(x - (float)hi[0], y - (float)hi[1]);
-        const f16x2_t g = __builtin_bit_cast(f16x2_t, (unsigned)qf[j][i]);
-        sum += (float)g[0] + (float)g[1];
+        const float x = v[i] * up;
+        const _Float16 g = (_Float16)x, r = FINE ? (_Float16)(x - (float)g) : (_Float16)0;
+        sum += (float)g + (float)r;
+        // codes of K that are not shifted stand at bits 4 to 7, 16 times as large
+        hi[2 * i] = __builtin_bit_cast(uint16_t, !FINE && (i & 1) ? (_Float16)(g * (_Float16)0.0625f) : g);
+        hi[2 * i + 64] = __builtin_bit_cast(uint16_t, r);
       }
-    sum = sum_column(sum);
-    Q = sum + dpp<0x128>(sum);
+      sum = sum16(sum);
+      if constexpr (TH == 32) sum += swz_xor16(sum);
+      if (threadIdx.x % TH == 0) {
+        sqf[0][h] = sum;
+        const float f = ldexpf(fabsf(a.scale) * 1.4426950408889634f, e - 13);
+        sqf[1][h] = f > 0.f ? f : 1.f;
+      }
+    }
   }
-  const unsigned lomask = col >= 8 ? 0xffffffffu : 0u;
+  __syncthreads();
+  u32x4 qf[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) qf[j] = *(const u32x4*)sq[j][lane + quad];
+  const float Q = sqf[0][col & 7], f = sqf[1][col & 7];  // sum of the head's q; a score's unit in powers of two
+  const unsigned part2 = col >= 8 ? 0xffffffffu : 0u;
 
   f32x4_t acc[2 * W];
 #pragma unroll
   for (int i = 0; i < 2 * W; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float M = -INFINITY, l = 0.f, mv = 0.f;
-  const int b0 = k0 >> 4;
-  auto block = [&](int b) { return sid[min(b - b0, kSplit4 / kBlock - 1)]; };
-  __syncthreads();
-  struct Tile { unsigned kw[4][W]; u32x4 vw[W]; unsigned ks, vs; };
-  auto load = [&](int t, Tile& x) {
-    const unsigned char* kp = pool + block(4 * t + (col >> 2)) * stride + (lane & 3) * (HD / 2) + quad * (HD / 8);
-    const unsigned char* vp = pool + block(4 * t + quad) * stride + 8 * HD + col * 16;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      if constexpr (W == 4) {
-        const u32x4 y = *(const u32x4*)(kp + n * 2 * HD);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x.kw[n][j] = y[j];
-      } else {
-        const u32x2_t y = *(const u32x2_t*)(kp + n * 2 * HD);
-        x.kw[n][0] = y[0]; x.kw[n][1] = y[1];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < W; ++i) x.vw[i] = *(const u32x4*)(vp + i * 256);
-    // this lane's key: slot col of block quad
-    x.ks = *(const unsigned*)(vp + 8 * HD - col * 12);
-    x.vs = *(const unsigned*)(vp + 8 * HD + 64 - col * 12);
-  };
-#if 1
-  Tile nxt;
-  load((k0 >> 6) + w, nxt);
-#endif
-  for (int t = (k0 >> 6) + w; t * 64 < k1; t += 4) {
-#if 1
-    const Tile cur = nxt;
-    load(t + 4, nxt);
-#else
-    Tile cur;
-    load(t, cur);
-#endif
-    const auto& kw = cur.kw;
-    const auto& vw = cur.vw;
-    unsigned ks = cur.ks, vs = cur.vs;
+  for (int t = t0; t * 64 < k1; t += 4) {
+    const int nb = min(4 * (t + 4) - b0, split / kBlock - 4);      // past the split: any tile
     if (64 * t + lane >= k1) ks = vs = 0;          // whatever lies behind the last key
-    *(float2*)&ssc[w][0][quad][2 * col] = make_float2(__uint_as_float(ks << 16) * 1048576.f, __uint_as_float(ks & 0xffff0000u));
+    *(float2*)&ssc[w][0][quad][2 * col] = make_float2(__uint_as_float(ks << 16) * (FINE ? 0x1p20f : 0x1p24f), __uint_as_float(ks & 0xffff0000u));
     *(float2*)&ssc[w][1][quad][2 * col] = make_float2(__uint_as_float(vs << 16), fmaf(__uint_as_float(vs << 16), FINE ? 8.f : 0.f, __uint_as_float(vs & 0xffff0000u)));
     wave_lds_fence();
 
-    float s[16];
+    f32x4_t d[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      f32x4_t d = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      d[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < W; ++j)
-        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, codes_f16(kw[n][j])),
-                                                   __builtin_bit_cast(f16x8_t, qf[j]), d, 0, 0, 0);
+        d[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, FINE ? codes_f16(kw[n][j]) : codes_mixed(kw[n][j])),
+                                                   __builtin_bit_cast(f16x8_t, qf[j]), d[n], 0, 0, 0);
+    }
+    load_k(sid[nb + (col >> 2)], sid[nb + quad]);
+    float s[16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 sm = *(const float2*)&ssc[w][0][quad][2 * (4 * n + i)];
-        s[4 * n + i] = fmaf(sm.x, d[i] + dpp<0x128>(d[i]), sm.y * Q);
-      }
+    for (int e = 0; e < 16; ++e) {
+      const float2 sm = *(const float2*)&ssc[w][0][quad][2 * e];
+      // without a lo part, columns past 7 are not used
+      const float x = FINE ? d[e >> 2][e & 3] + dpp<0x128>(d[e >> 2][e & 3]) : d[e >> 2][e & 3];
+      s[e] = fmaf(sm.x, x, sm.y * Q);
     }
     if (64 * t + 64 > k1) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (64 * t + 16 * quad + e >= k1) s[e] = -INFINITY;
     }
-    float pv[16], sv[16], ts, tm, pm;
+    float pv[16], ts, tm, pm;
     auto probabilities = [&] {
       ts = tm = pm = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float p = __builtin_amdgcn_exp2f(fmaf(s[e], f, -M));
         const float2 sm = *(const float2*)&ssc[w][1][quad][2 * e];
-        sv[e] = sm.x;
         pv[e] = p * sm.x;
         ts += p;
         tm = fmaf(p, sm.y, tm);
@@ -564,13 +560,14 @@ __global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, con
     const bool first = __any(M == -INFINITY);
     if (!first) probabilities();
     if (first || !__all(pm <= 8192.f && ts < INFINITY)) {
-      float u = -INFINITY;
+      float u = -INFINITY, big = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float2 sm = *(const float2*)&ssc[w][1][quad][2 * e];
-        u = fmaxf(u, fmaf(s[e], f, fmaxf(__builtin_amdgcn_logf(sm.x), -90.f)));
+        u = fmaxf(u, s[e]);
+        big = fmaxf(big, ssc[w][1][quad][2 * e]);
       }
-      u = fmaxf(max_column(u) - 8.f, M);
+      u = fmaf(max_column(u), f, fmaxf(__builtin_amdgcn_logf(max_column(big)), -90.f));
+      u = fmaxf(u - 8.f, M);
       const float alpha = __builtin_amdgcn_exp2f(M - u);
       M = u;
       l *= alpha;
@@ -588,8 +585,12 @@ __global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, con
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = 8 * h + 4 * (i >> 1) + (i & 1);
-        const f16x2_t hi = __builtin_bit_cast(f16x2_t, pack_f16(pv[e], pv[e + 2]) & lomask);
-        pf[i] = pack_f16(pv[e] - (float)hi[0], pv[e + 2] - (float)hi[1]);
+        if constexpr (FINE) {
+          const f16x2_t hi = __builtin_bit_cast(f16x2_t, pack_f16(pv[e], pv[e + 2]) & part2);
+          pf[i] = pack_f16(pv[e] - (float)hi[0], pv[e + 2] - (float)hi[1]);
+        } else {
+          pf[i] = pack_f16(pv[e], pv[e + 2]) & ~part2;
+        }
       }
 #pragma unroll
       for (int i = 0; i < W; ++i) {
@@ -606,6 +607,7 @@ __global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, con
         acc[W + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, hi), __builtin_bit_cast(f16x8_t, pf), acc[W + i], 0, 0, 0);
       }
     }
+    load_v(sid[nb + quad]);
     wave_lds_fence();
   }
 
@@ -617,7 +619,7 @@ __global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, con
   for (int i = 0; i < 2 * W; ++i) {
     f32x4_t o;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = fmaf(acc[i][k] + dpp<0x128>(acc[i][k]), FINE ? 1.f : 1048576.f, mv);
+    for (int k = 0; k < 4; ++k) o[k] = fmaf(acc[i][k] + dpp<0x128>(acc[i][k]), FINE ? 1.f : 0x1p20f, mv);
     if (col < gq) *(f32x4_t*)&so[w][col][16 * i + 4 * quad] = o;
   }
   __syncthreads();
@@ -648,27 +650,33 @@ __global__ __launch_bounds__(256, A4_WPE) void k_attend4_rows(Attend4Args a, con
   }
 }
 
-// The join of a row's splits, in their order.
+// The join of a row's splits, in their order: a workgroup a row and KV head, four dims a thread.
 template <int HD>
-__global__ __launch_bounds__(HD) void k_attend4_join(Attend4Args a, Partial4 part) {
-  const int row = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+__global__ __launch_bounds__(256) void k_attend4_join(Attend4Args a, int split, Partial4 part) {
+  const int row = blockIdx.x, gq = a.n_h / a.n_kv;
   const int seq = a.row_seq[row];
   const int ctx = (unsigned)seq < (unsigned)a.n_seqs ? min(a.row_ctx[row], a.max_ctx) : 0;
-  if (ctx <= kSplit4) return;
-  const int n = (ctx + kSplit4 - 1) / kSplit4;
-  float M = -INFINITY, l = 0.f, o = 0.f;
+  const int h = blockIdx.y * gq + threadIdx.x / (HD / 4), d = threadIdx.x % (HD / 4) * 4;
+  if (ctx <= split || threadIdx.x >= gq * (HD / 4)) return;
+  const int n = (ctx + split - 1) / split;
+  float M = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int s = 0; s < n; ++s) {
     const size_t b = ((size_t)s * a.T + row) * a.n_h + h;
-    const float ms = part.ml[2 * b], ls = part.ml[2 * b + 1], as = part.acc[b * HD + d];
-    const float mn = fmaxf(M, ms), x = __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(ms - mn);
-    l = l * x + ls * y;
-    o = o * x + as * y;
+    const float2 ml = *(const float2*)(part.ml + 2 * b);
+    const f32x4_t as = *(const f32x4_t*)(part.acc + b * HD + d);
+    const float mn = fmaxf(M, ml.x), x = __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(ml.x - mn);
+    l = l * x + ml.y * y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = o[k] * x + as[k] * y;
     M = mn;
   }
   const size_t at = ((size_t)row * a.n_h + h) * HD + d;
-  if (a.out_type == OUT_F32) ((float*)a.out)[at] = o / l;
-  else ((uint16_t*)a.out)[at] = f2bf(o / l);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] /= l;
+  if (a.out_type == OUT_F32) *(f32x4_t*)((float*)a.out + at) = o;
+  else *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
 }
 
 // =============================================================== launchers
@@ -709,29 +717,38 @@ hipError_t launch_kv_read(hipStream_t st, int kind, const void* kv, int layer, i
   return hipGetLastError();
 }
 
-static int splits4(int max_ctx) { return (max_ctx + kSplit4 - 1) / kSplit4; }
+// Keys per split: the longest of 2,048, 1,024 and 512 that gives every CU a workgroup. us at
+// 8 KV heads of 128, splits of 512, 1,024, 2,048: 256 rows of 4,000 keys 271, 223, 196; 16 of
+// 8,000 37.2, 32.5, 29.9; 16 of 2,000 14.0, 14.0, 15.9; 1 of 32,000 20.8, 17.4, 19.4; 1 of 4,000 10.9,
+// 12.5, 18.2; 256 keys: 10.5 there, but 20.0 where 512 take 14.9 (4 of 8,000).
+static int split4(int n_kv, int T, int max_ctx) {
+  int s = kSplit4Max;
+  while (s > 512 && (long long)T * n_kv * ((max_ctx + s - 1) / s) < 256) s /= 2;
+  return s;
+}
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-size_t attend4_rows_bytes(int n_h, int hd, int T, int max_ctx) {
-  const size_t slots = splits4(max_ctx) > 1 ? (size_t)T * splits4(max_ctx) : 0;
+size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx) {
+  const int s = split4(n_kv, T, max_ctx), n = (max_ctx + s - 1) / s;
+  const size_t slots = n > 1 ? (size_t)T * n : 0;
   return up256(slots * n_h * hd * 4) + slots * n_h * 8;
 }
 size_t attend4_chunks_bytes(int, int, int, int, int, int) { return 0; }
 
 hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace) {
   if (a.T <= 0) return hipSuccess;
-  const int n = splits4(a.max_ctx);
+  const int s = split4(a.n_kv, a.T, a.max_ctx), n = (a.max_ctx + s - 1) / s;
   if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)a.T * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
   Partial4 part{(float*)workspace, (float*)((char*)workspace + up256((size_t)a.T * n * a.n_h * a.hd * 4))};
   const dim3 grid((unsigned)(a.T * n * a.n_kv)), blk(256);
   const bool vec = a.q_stride % (a.q_bf16 ? 8 : 4) == 0 && (uintptr_t)a.q % 16 == 0;
-  auto go = [&](auto kern) { klaunch(kern, grid, blk, st, a, (const AttnItem*)nullptr, part, vec); };
+  auto go = [&](auto kern) { klaunch(kern, grid, blk, st, a, (const AttnItem*)nullptr, s, part, vec); };
   if (a.hd == 64) a.q_bf16 ? go(k_attend4_rows<64, false, false>) : go(k_attend4_rows<64, false, true>);
   else a.q_bf16 ? go(k_attend4_rows<128, false, false>) : go(k_attend4_rows<128, false, true>);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || n == 1) return err;
-  if (a.hd == 64) klaunch(k_attend4_join<64>, dim3(a.T, a.n_h), dim3(64), st, a, part);
-  else klaunch(k_attend4_join<128>, dim3(a.T, a.n_h), dim3(128), st, a, part);
+  if (a.hd == 64) klaunch(k_attend4_join<64>, dim3(a.T, a.n_kv), blk, st, a, s, part);
+  else klaunch(k_attend4_join<128>, dim3(a.T, a.n_kv), blk, st, a, s, part);
   return hipGetLastError();
 }
 

@@ -240,7 +240,7 @@ struct Attend4Args {
 };
 hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace);
 hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* workspace);
-size_t attend4_rows_bytes(int n_h, int hd, int T, int max_ctx);
+size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx);
 size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx);
 
 constexpr int kMaxTop = 32;

@@ -147,7 +147,7 @@ moa_status moa_kv_read(const moa_kv_cfg* c, const void* kv, int32_t layer, int32
 
 moa_status moa_kv_attend_bytes(const moa_kv_cfg* c, int32_t n_rows, int32_t max_ctx, size_t* bytes) {
   if (!valid_kv(c) || c->kind != MOA_KV_INT4 || n_rows < 0 || max_ctx < 1 || !bytes) return MOA_EINVAL;
-  *bytes = attend4_rows_bytes(c->n_heads, c->head_dim, n_rows, max_ctx);
+  *bytes = attend4_rows_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, max_ctx);
   return MOA_OK;
 }
 
@@ -159,7 +159,7 @@ moa_status moa_kv_attend(const moa_kv_cfg* c, const void* kv, int32_t layer, con
   if (st != MOA_OK) return st;
   if (n_rows == 0) return MOA_OK;
   if (!aligned(row_seq, 4) || !aligned(row_ctx, 4)) return MOA_EINVAL;
-  st = check_workspace(workspace, workspace_bytes, attend4_rows_bytes(c->n_heads, c->head_dim, n_rows, max_ctx));
+  st = check_workspace(workspace, workspace_bytes, attend4_rows_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, max_ctx));
   if (st != MOA_OK) return st;
   Attend4Args a = attend_args(c, kv, layer, q, type, q_stride, n_rows, tables, n_seqs, table_len, max_ctx, scale, out);
   a.row_seq = row_seq;
