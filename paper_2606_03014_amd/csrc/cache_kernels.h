@@ -247,63 +247,6 @@ __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, in
   }
 }
 
-// ------------------------------------------- attention over 4-bit cells, one wave
-// a row and query head: key after key, lane l holding dims l (and l + 64).
-template <int HD>
-__global__ __launch_bounds__(64) void k_attend4(Attend4Args a) {
-  constexpr int N = HD / 64;
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  int seq, ctx;
-  if (a.chunk_start) {
-    seq = -1;
-    for (int i = 0; i < a.n_seqs; ++i)
-      if (t >= a.chunk_start[i] && t < a.chunk_start[i + 1]) seq = i;
-    if (seq < 0) return;
-    ctx = min(a.chunk_ctx[seq], a.max_ctx) - (a.chunk_start[seq + 1] - 1 - t);
-  } else {
-    seq = a.row_seq[t];
-    ctx = (unsigned)seq < (unsigned)a.n_seqs ? min(a.row_ctx[t], a.max_ctx) : 0;
-  }
-  const int kh = h / (a.n_h / a.n_kv);
-  float q[N], o[N], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const size_t at = (size_t)t * a.q_stride + (size_t)h * HD + lane + 64 * i;
-    q[i] = (a.q_bf16 ? load_el<true>(a.q, at) : load_el<false>(a.q, at)) * a.scale;
-    o[i] = 0.f;
-  }
-  for (int j = 0; j < ctx; ++j) {
-    const unsigned b = min((unsigned)a.tables[(size_t)seq * a.table_len + (j >> 4)], (unsigned)a.num_blocks - 1);
-    const unsigned char* cell = kv_cell(a.kv, KV_INT4, HD, a.layer, a.num_blocks, (int)b, a.n_kv, kh);
-    const int slot = j & 15;
-    const unsigned ks = ((const unsigned*)(cell + 16 * HD))[slot], vs = ((const unsigned*)(cell + 16 * HD))[16 + slot];
-    float dot = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int d = lane + 64 * i, c = (cell[slot * (HD / 2) + (d >> 1)] >> (4 * (d & 1))) & 15;
-      dot = fmaf(q[i], fmaf(__uint_as_float(ks << 16), (float)c, __uint_as_float(ks & 0xffff0000u)), dot);
-    }
-    dot = wave_sum(dot);
-    const float mn = fmaxf(m, dot), alpha = __expf(m - mn), p = __expf(dot - mn);
-    m = mn;
-    l = l * alpha + p;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int d = lane + 64 * i, half = d / (HD / 2);
-      const int c = (cell[8 * HD + (d - half * (HD / 2)) * 16 + slot] >> (4 * half)) & 15;
-      o[i] = o[i] * alpha + p * fmaf(__uint_as_float(vs << 16), (float)c, __uint_as_float(vs & 0xffff0000u));
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const size_t at = ((size_t)t * a.n_h + h) * HD + lane + 64 * i;
-    const float r = ctx > 0 ? o[i] / l : 0.f;
-    if (a.out_type == OUT_F32) ((float*)a.out)[at] = r;
-    else if (a.out_type == OUT_BF16) ((uint16_t*)a.out)[at] = f2bf(r);
-    else store_split((uint16_t*)a.out, a.out_lo, at, r);
-  }
-}
-
 // ---------------------------- decode attention over 4-bit cells (16x16x32 MFMA)
 // One workgroup is a row, a KV head and one split of its keys; its four waves take
 // every fourth tile of 64 keys (four blocks) and join at the end.
@@ -679,6 +622,354 @@ __global__ __launch_bounds__(256) void k_attend4_join(Attend4Args a, int split, 
   else *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
 }
 
+// ------------------------- causal chunk attention over 4-bit cells (32x32x16 MFMA)
+// One workgroup is 128 queries of one chunk and KV head: 128 / gq positions of its gq query
+// heads, side by side, so short chunks fill the tile too; a wave has 32 of them.
+// Tiles of 64 keys are unpacked once for the four waves: each thread brings 16 bytes of K
+// codes and 16 of V, a tile ahead of its unpacking and two ahead of their use, and
+// writes them as float16 codes (as in k_attend4_rows) to LDS in the order of the MFMA
+// operands, where V's [dim][slot] cells need no transposing. Two LDS buffers, one barrier a
+// tile. S^T = K Q^T: row 8 a + 4 h + i of a 32-key score tile is block a / 2, slot
+// 8 h + 4 (a % 2) + i, so lane half h ends with slots 8 h .. + 8 of both blocks, the k-slots of
+// O^T = V^T P^T. Scales, minima, the reference M and float16 pairs as in k_attend4_rows;
+// in bf16 calls q is one exact float16 and P one float16, half the products.
+struct Chunk { int row0, nq, pos0; const int* tab; };
+
+// The block of 128 / gq rows that workgroup slot b stands for: chunk i has the slots
+// start_i / PB + i and on, which never meet the next chunk's. nq = 0: none.
+__device__ __forceinline__ Chunk find_chunk(const Attend4Args& a, int b, int PB) {
+  int n = 0;
+  for (int i0 = 0; i0 < a.n_seqs; i0 += 256) {
+    const int i = i0 + threadIdx.x;
+    n += __syncthreads_count(i < a.n_seqs && a.chunk_start[min(i, a.n_seqs)] / PB + i <= b);
+  }
+  Chunk c{0, 0, 0, nullptr};
+  const int i = n - 1;
+  if (i < 0) return c;
+  const int s0 = max(a.chunk_start[i], 0), s1 = min(a.chunk_start[i + 1], a.T);
+  const int r0 = s0 + (b - (s0 / PB + i)) * PB;
+  c.row0 = r0;
+  c.nq = max(min(PB, s1 - r0), 0);
+  c.pos0 = min(a.chunk_ctx[i], a.max_ctx) - (s1 - r0);
+  c.tab = a.tables + (size_t)i * a.table_len;
+  return c;
+}
+
+__device__ __forceinline__ void store_out4(const Attend4Args& a, size_t at, f32x4_t o) {
+  if (a.out_type == OUT_F32) {
+    *(f32x4_t*)((float*)a.out + at) = o;
+  } else if (a.out_type == OUT_BF16) {
+    *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+  } else {
+    unsigned h0, h1, l0, l1;
+    split_pair(o[0], o[1], h0, l0);
+    split_pair(o[2], o[3], h1, l1);
+    *(uint2*)((uint16_t*)a.out + at) = make_uint2(h0, h1);
+    *(uint2*)((uint16_t*)a.out + a.out_lo + at) = make_uint2(l0, l1);
+  }
+}
+
+template <int HD, bool ITEMS, bool FINE>
+__global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const PrefillItem* __restrict__ items, int nslots,
+                                                           int split, Partial4 part, bool q_vec) {
+  constexpr int CELL = (int)kv_cell_bytes(KV_INT4, HD);
+  constexpr int DS = HD / 16, DT = HD / 32;        // 16-dim steps of the scores, 32-dim tiles of the answer
+  constexpr int W = HD / 32;                       // words of a key's row per wave
+  constexpr int KB = 64 * HD * 2;                  // bytes of a tile's K (and V) as float16
+  extern __shared__ __align__(1024) unsigned char lds[];
+  float* ssc = (float*)(lds + 4 * KB);             // [buffer][K, V][64 keys] (s, m)
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hf = lane >> 5, gq = a.n_h / a.n_kv, kvh = blockIdx.x % a.n_kv;
+  const int item = blockIdx.x / a.n_kv, PB = 128 / gq;
+  const int sp = item / nslots, b = nslots - 1 - (item - sp * nslots);    // late positions, long ones, first
+  Chunk c;
+  if constexpr (ITEMS) {
+    const PrefillItem it = items[b];
+    c = Chunk{it.row0, it.nq, it.pos0, a.tables + it.bt_off};
+  } else {
+    c = find_chunk(a, b, PB);
+  }
+  if (c.nq == 0) return;
+  const int kmax = c.pos0 + c.nq;                  // keys [0, kmax)
+  const int k0 = sp * split, k1 = min(kmax, k0 + split);
+  // this lane's query (those past nq repeat the last row's and are never stored)
+  const int slot = min(32 * w + c32, c.nq * gq - 1), r = slot / gq, h = kvh * gq + slot - r * gq;
+  const bool mine = 32 * w + c32 < c.nq * gq;
+  const int qpos = c.pos0 + r;
+  const size_t orow = (size_t)(c.row0 + r) * a.n_h + h;
+  const size_t prow = ((size_t)sp * a.T + c.row0 + r) * a.n_h + h;
+  if (k0 >= k1) {                                  // no key of this split, or none at all
+    if (part.ml) {
+      if (mine && hf == 0) *(float2*)(part.ml + 2 * prow) = make_float2(-INFINITY, 0.f);
+    } else if (mine) {
+      for (int d = 4 * hf; d < HD; d += 8) store_out4(a, orow * HD + d, f32x4_t{0.f, 0.f, 0.f, 0.f});
+    }
+    return;
+  }
+  const unsigned char* pool = (const unsigned char*)a.kv + ((size_t)a.layer * a.num_blocks * a.n_kv + kvh) * CELL;
+  const size_t stride = (size_t)a.n_kv * CELL;
+  const int last = (kmax - 1) >> 4;
+  auto id_of = [&](int x) { return min((unsigned)c.tab[min(x, last)], (unsigned)a.num_blocks - 1u); };
+
+  // staging: thread (w, lane) brings words W w .. of key `lane`'s row, and the 16 slots of dim `lane` (and
+  // + HD / 2) of block w; threads below 128 one scale word (K of keys 0 .. 63, then V)
+  const int vb = HD == 128 ? w : threadIdx.x >> 5, vd = HD == 128 ? lane : lane & 31;
+  const bool has_v = HD == 128 || w < 2, has_s = w < 2;
+  unsigned kid, vid;
+  auto ids = [&](int t) {
+    kid = id_of(4 * t + (lane >> 4));
+    vid = id_of(4 * t + min(vb, 3));
+  };
+  unsigned kw[W], sw;
+  u32x4 vw;
+  auto load = [&](int t) {
+    const unsigned char* cell = pool + kid * stride;
+    if constexpr (W == 4) {
+      const u32x4 x = *(const u32x4*)(cell + (lane & 15) * (HD / 2) + w * 16);
+      kw[0] = x[0]; kw[1] = x[1]; kw[2] = x[2]; kw[3] = x[3];
+    } else {
+      const u32x2_t x = *(const u32x2_t*)(cell + (lane & 15) * (HD / 2) + w * 8);
+      kw[0] = x[0]; kw[1] = x[1];
+    }
+    if (has_s) {
+      sw = *(const unsigned*)(cell + 16 * HD + 64 * w + 4 * (lane & 15));
+      if (64 * t + lane >= kmax) sw = 0;           // whatever lies behind the last key
+    }
+    if (has_v) vw = *(const u32x4*)(pool + vid * stride + 8 * HD + vd * 16);
+  };
+  // row of the score tile that key `lane` takes
+  const int krow = 8 * (2 * ((lane >> 4) & 1) + ((lane >> 2) & 1)) + 4 * ((lane >> 3) & 1) + (lane & 3);
+  auto unpack = [&](int t) {
+    unsigned char* kb = lds + (t & 1) * KB;
+    unsigned char* vbuf = lds + 2 * KB + (t & 1) * KB;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      const int x = W * w + j;                     // the word's dims: step x / 2, half x % 2
+      *(u32x4*)(kb + (((lane >> 5) * DS + (x >> 1)) * 64 + (x & 1) * 32 + krow) * 16) = codes_f16(kw[j]);
+    }
+    if (has_v) {
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const unsigned x = vw[2 * o], y = vw[2 * o + 1];
+        u32x4 lo, hi;
+        if constexpr (FINE) {
+          lo = u32x4{centred(x << 6), centred(x >> 2), centred(y << 6), centred(y >> 2)};
+          hi = u32x4{centred(x << 2), centred(x >> 6), centred(y << 2), centred(y >> 6)};
+        } else {
+          lo = u32x4{(x << 4) & kCodeMask, (x >> 4) & kCodeMask, (y << 4) & kCodeMask, (y >> 4) & kCodeMask};
+          hi = u32x4{x & kCodeMask, (x >> 8) & kCodeMask, y & kCodeMask, (y >> 8) & kCodeMask};
+        }
+        unsigned char* f = vbuf + ((vb * DT + (vd >> 5)) * 64 + o * 32 + (vd & 31)) * 16;
+        *(u32x4*)f = lo;
+        *(u32x4*)(f + DT / 2 * 1024) = hi;
+      }
+    }
+    if (has_s) {
+      const float s = __uint_as_float(sw << 16), m = __uint_as_float(sw & 0xffff0000u);
+      *(float2*)&ssc[((t & 1) * 128 + 64 * w + lane) * 2] =
+          w == 0 ? make_float2(s * 0x1p20f, m) : make_float2(s, FINE && s == s ? fmaf(s, 8.f, m) : m);
+    }
+  };
+
+  // B operand of the scores: query `slot`, dims 16 s + 8 hf .. + 8 in the order of codes_f16
+  u32x4 qh[DS], ql[FINE ? DS : 1];
+  float Q, f;
+  {
+    float v[DS][8], mx = 0.f;
+    const size_t qo = (size_t)(c.row0 + r) * a.q_stride + (size_t)h * HD + 8 * hf;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+      load_run<8>(a.q, qo + 16 * s, a.q_bf16, q_vec, v[s]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[s][i]));
+    }
+    mx = max_halves(mx);
+    int e = 0;
+    if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
+    const float up = a.scale > 0.f ? ldexpf(1.f, 13 - e) : (a.scale < 0.f ? -ldexpf(1.f, 13 - e) : 0.f);
+    f = ldexpf(fabsf(a.scale) * 1.4426950408889634f, e - 13);
+    if (!(f > 0.f)) f = 1.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < DS; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = v[s][i] * up, y = v[s][i + 4] * up;
+        qh[s][i] = pack_f16(x, y);
+        const f16x2_t g = __builtin_bit_cast(f16x2_t, (unsigned)qh[s][i]);
+        sum += (float)g[0] + (float)g[1];
+        if constexpr (FINE) {
+          ql[s][i] = pack_f16(x - (float)g[0], y - (float)g[1]);
+          const f16x2_t k = __builtin_bit_cast(f16x2_t, (unsigned)ql[s][i]);
+          sum += (float)k[0] + (float)k[1];
+        }
+      }
+    Q = add_halves(sum);
+  }
+
+  f32x16_t O[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) O[d] = f32x16_t{};
+  float M = -INFINITY, l = 0.f, mv = 0.f;
+  const int ta = k0 >> 6, tb = (k1 + 63) >> 6;     // tiles
+  const int first_pos = c.pos0 + min(32 * w, c.nq * gq - 1) / gq;
+  ids(ta);
+  load(ta);
+  ids(ta + 1);
+  unpack(ta);
+  load(ta + 1);
+  ids(ta + 2);
+  __syncthreads();
+  for (int t = ta; t < tb; ++t) {
+    const unsigned char* kb = lds + (t & 1) * KB;
+    const unsigned char* vbuf = lds + 2 * KB + (t & 1) * KB;
+    f32x16_t S[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      S[k] = f32x16_t{};
+#pragma unroll
+      for (int s = 0; s < DS; ++s) {
+        const f16x8_t x = __builtin_bit_cast(f16x8_t, *(const u32x4*)(kb + ((k * DS + s) * 64 + lane) * 16));
+        S[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, qh[s]), S[k], 0, 0, 0);
+        if constexpr (FINE) S[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, ql[s]), S[k], 0, 0, 0);
+      }
+    }
+    const bool masked = 64 * t + 63 > first_pos;   // some query of the wave does not see the whole tile
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      // element e: key 64 t + 32 k + 16 (e / 8) + 8 hf + e % 8
+      const float* kc = ssc + ((t & 1) * 128 + 32 * k + 8 * hf) * 2;
+      const float* vc = kc + 128;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float2 sm = *(const float2*)(kc + (16 * (e >> 3) + (e & 7)) * 2);
+        S[k][e] = fmaf(sm.x, S[k][e], sm.y * Q);
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (64 * t + 32 * k + 16 * (e >> 3) + 8 * hf + (e & 7) > qpos) S[k][e] = -INFINITY;
+      }
+      float pv[16], ts, tm, pm;
+      auto probabilities = [&](float base) {
+        ts = tm = pm = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(S[k][e], f, -base));
+          const float2 sm = *(const float2*)(vc + (16 * (e >> 3) + (e & 7)) * 2);
+          pv[e] = p * sm.x;
+          ts += p;
+          tm = fmaf(p, sm.y, tm);
+          pm = fmaxf(pm, pv[e]);
+        }
+      };
+      const bool first = __any(M == -INFINITY);    // also while a query has not met a key
+      if (!first) probabilities(M);
+      if (first || !__all(pm <= 8192.f && ts < INFINITY)) {
+        float u = -INFINITY, big = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          u = fmaxf(u, S[k][e]);
+          big = fmaxf(big, vc[(16 * (e >> 3) + (e & 7)) * 2]);
+        }
+        u = fmaf(max_halves(u), f, fmaxf(__builtin_amdgcn_logf(max_halves(big)), -90.f));
+        u = fmaxf(u - 8.f, M);
+        const float alpha = M == u ? 1.f : __builtin_amdgcn_exp2f(M - u);
+        M = u;
+        l *= alpha;
+        mv *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[d] *= alpha;
+        probabilities(M == -INFINITY ? 0.f : M);
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (S[k][e] == -INFINITY) pv[e] = 0.f;   // also where the unseen row stands for NaN
+        // (its minimum is finite: it adds 0 to the sums)
+      }
+      l += ts;
+      mv += tm;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        u32x4 ph, pl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 8 * u + 4 * (i >> 1) + (i & 1);
+          ph[i] = pack_f16(pv[e], pv[e + 2]);
+          if constexpr (FINE) {
+            const f16x2_t g = __builtin_bit_cast(f16x2_t, (unsigned)ph[i]);
+            pl[i] = pack_f16(pv[e] - (float)g[0], pv[e + 2] - (float)g[1]);
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const f16x8_t x = __builtin_bit_cast(f16x8_t, *(const u32x4*)(vbuf + (((2 * k + u) * DT + d) * 64 + lane) * 16));
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, ph), O[d], 0, 0, 0);
+          if constexpr (FINE) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, pl), O[d], 0, 0, 0);
+        }
+      }
+    }
+    if (t + 1 < tb) {
+      unpack(t + 1);
+      load(t + 2);
+      ids(t + 3);
+    }
+    __syncthreads();
+  }
+
+  l = add_halves(l);
+  mv = add_halves(mv);
+  if (!mine) return;
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;       // a query at a negative position: 0
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      f32x4_t o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = fmaf(O[d][e + i], FINE ? 1.f : 0x1p20f, mv);
+      const int dim = 32 * d + 2 * e + 4 * hf;
+      if (part.ml) {
+        *(f32x4_t*)(part.acc + prow * HD + dim) = o;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= inv;
+        store_out4(a, orow * HD + dim, o);
+      }
+    }
+  if (part.ml && hf == 0) *(float2*)(part.ml + 2 * prow) = make_float2(M, l);
+}
+
+// The join of a chunk's splits, in their order: a workgroup per block of rows and KV head.
+template <int HD>
+__global__ __launch_bounds__(256) void k_attend4_chunks_join(Attend4Args a, int nsplit, Partial4 part) {
+  const int gq = a.n_h / a.n_kv, PB = 128 / gq;
+  const Chunk c = find_chunk(a, blockIdx.x, PB);
+  constexpr int TR = HD / 4;                       // threads a row and head
+  for (int i = threadIdx.x / TR; i < c.nq * gq; i += 256 / TR) {
+    const size_t row = (size_t)(c.row0 + i / gq) * a.n_h + blockIdx.y * gq + i % gq;
+    const int d = threadIdx.x % TR * 4;
+    float M = -INFINITY, l = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < nsplit; ++s) {
+      const size_t b = (size_t)s * a.T * a.n_h + row;
+      const float2 ml = *(const float2*)(part.ml + 2 * b);
+      if (ml.x == -INFINITY) continue;             // nothing seen in this split: nothing was written
+      const f32x4_t as = *(const f32x4_t*)(part.acc + b * HD + d);
+      const float mn = fmaxf(M, ml.x), x = __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(ml.x - mn);
+      l = l * x + ml.y * y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = o[k] * x + as[k] * y;
+      M = mn;
+    }
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] *= inv;
+    store_out4(a, row * HD + d, o);
+  }
+}
+
 // =============================================================== launchers
 
 hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a) {
@@ -733,7 +1024,6 @@ size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx) {
   const size_t slots = n > 1 ? (size_t)T * n : 0;
   return up256(slots * n_h * hd * 4) + slots * n_h * 8;
 }
-size_t attend4_chunks_bytes(int, int, int, int, int, int) { return 0; }
 
 hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace) {
   if (a.T <= 0) return hipSuccess;
@@ -752,12 +1042,47 @@ hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* works
   return hipGetLastError();
 }
 
-static hipError_t attend4(hipStream_t st, const Attend4Args& a) {
+// Workgroup slots and key splits of a chunk call: splits (of whole tiles, at least 512 keys)
+// only where the blocks of rows leave CUs without a workgroup.
+static void plan_chunks4(int n_h, int n_kv, int T, int n_chunks, int max_ctx, int& nslots, int& split, int& nsplit) {
+  nslots = T / (128 / (n_h / n_kv)) + n_chunks;
+  const long long wgs = (long long)nslots * n_kv;
+  nsplit = (int)std::max(1ll, std::min((512 + wgs - 1) / wgs, (long long)max_ctx / 512));
+  split = ((max_ctx + nsplit - 1) / nsplit + 63) / 64 * 64;
+  nsplit = (max_ctx + split - 1) / split;
+}
+
+size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx) {
+  int nslots, split, n;
+  plan_chunks4(n_h, n_kv, T, n_chunks, max_ctx, nslots, split, n);
+  return n > 1 ? up256((size_t)n * T * n_h * hd * 4) + (size_t)n * T * n_h * 8 : 0;
+}
+
+hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* workspace) {
   if (a.T <= 0) return hipSuccess;
-  const dim3 grid(a.T, a.n_h), blk(64);
-  if (a.hd == 64) klaunch(k_attend4<64>, grid, blk, st, a);
-  else if (a.hd == 128) klaunch(k_attend4<128>, grid, blk, st, a);
-  else return hipErrorInvalidValue;
+  int nslots, split, n;
+  plan_chunks4(a.n_h, a.n_kv, a.T, a.n_seqs, a.max_ctx, nslots, split, n);
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)nslots * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
+  Partial4 part{nullptr, nullptr};
+  if (n > 1) part = {(float*)workspace, (float*)((char*)workspace + up256((size_t)n * a.T * a.n_h * a.hd * 4))};
+  const unsigned shm = 4u * 64u * (unsigned)a.hd * 2u + 2048u;
+  const bool vec = a.q_stride % (a.q_bf16 ? 8 : 4) == 0 && (uintptr_t)a.q % 16 == 0;
+  static bool attr = false;                // one attribute call per process for the instantiations
+  if (!attr) {
+    for (const void* f : {(const void*)k_attend4_chunks<64, false, false>, (const void*)k_attend4_chunks<64, false, true>,
+                          (const void*)k_attend4_chunks<128, false, false>, (const void*)k_attend4_chunks<128, false, true>}) {
+      const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * 64 * 128 * 2 + 2048);
+      if (e != hipSuccess) return e;
+    }
+    attr = true;
+  }
+  const dim3 grid((unsigned)(nslots * n * a.n_kv)), blk(256);
+  auto go = [&](auto kern) { klaunch_shm(kern, grid, blk, shm, st, a, (const PrefillItem*)nullptr, nslots, split, part, vec); };
+  if (a.hd == 64) a.q_bf16 ? go(k_attend4_chunks<64, false, false>) : go(k_attend4_chunks<64, false, true>);
+  else a.q_bf16 ? go(k_attend4_chunks<128, false, false>) : go(k_attend4_chunks<128, false, true>);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || n == 1) return err;
+  if (a.hd == 64) klaunch(k_attend4_chunks_join<64>, dim3(nslots, a.n_kv), blk, st, a, n, part);
+  else klaunch(k_attend4_chunks_join<128>, dim3(nslots, a.n_kv), blk, st, a, n, part);
   return hipGetLastError();
 }
-hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void*) { return attend4(st, a); }

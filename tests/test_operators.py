@@ -485,6 +485,49 @@ def test_chunks_before_the_first_position_and_sharp_ones(ops, hd):
     check_out(out[10:190], want, A, max(float(v.abs().max()) for v in p.v), F, f"sharp chunks {hd}")
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_nan_row_reaches_only_later_rows_of_a_chunk(ops, hd, dtype):
+    p = Pool(ops, [150, 70], 2, 2, hd, seed=9)
+    for col in (4, 6):                                           # keys of head 0, values of head 0
+        x = torch.zeros(1, 8 * hd)
+        x[0, col * hd + 3] = math.nan
+        p.kv.append(0, x.cuda(), i32([0]), i32([90 + col]), p.tables)      # the head's other rows stand for 0
+    q = torch.randn(220, 4, hd, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    out = p.kv.attend_chunks(0, q, i32([0, 150, 220]), i32([150, 70]), p.tables, 150)
+    assert torch.isfinite(out[150:]).all() and torch.isfinite(out[:94]).all() and torch.isfinite(out[:, 2:]).all()
+    assert out[94:150, :2].isnan().all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("hd,gq", [(64, 4), (128, 2)])
+def test_few_rows_behind_long_contexts(ops, hd, gq, dtype):
+    """Grids that are split over the keys: chunks whose first rows see none of the later splits, an empty one."""
+    lens, ctx = [3, 0, 40, 1], [2900, 5, 41, 513]
+    p = Pool(ops, ctx, 1, gq, hd, seed=5)
+    q = torch.randn(44, gq, hd, generator=torch.Generator().manual_seed(4)).to(dtype).cuda()
+    out = torch.full_like(q, 3.0)
+    out = p.kv.attend_chunks(0, q, i32([0, 3, 3, 43, 44]), i32(ctx), p.tables, 16 * p.tables.shape[1], out=out)
+    want, A = chunk_want(p, q, lens, ctx, hd)
+    rel = check_out(out, want, A, max(float(v.abs().max()) for v in p.v if len(v)), dtype, f"long {hd} {dtype}")
+    assert rel <= (2.0 ** -16 if dtype == F else 2.0 ** -8)
+
+
+@gpu
+@pytest.mark.parametrize("hd", [64, 128])
+def test_decode_rows_in_long_splits(ops, hd):
+    """Enough rows for splits of 2,048 keys: rows that end on, before and behind one."""
+    n = [2047, 2048, 2049, 4096, 4500, 64, 1]
+    p = Pool(ops, n, 1, 1, hd, seed=6)
+    seq = [i % 7 for i in range(300)]
+    q = torch.randn(300, 1, hd, generator=torch.Generator().manual_seed(4))
+    out = p.kv.attend(0, q.cuda(), i32(seq), i32([n[i] for i in seq]), p.tables, 4500).cpu()
+    want, A = zip(*(attention(q[r].double(), p.k[b], p.v[b], hd ** -0.5) for r, b in enumerate(seq)))
+    assert check_out(out, torch.stack(want), max(A), max(float(v.abs().max()) for v in p.v), F, "long splits") <= 2.0 ** -16
+
+
 # ------------------------------------------------------------------ scores
 
 def score_want(x, tok, k):
