@@ -628,8 +628,7 @@ __global__ __launch_bounds__(256) void k_attend4_join(Attend4Args a, int split, 
 // Tiles of 64 keys are unpacked once for the four waves: each thread brings 16 bytes of K
 // codes and 16 of V, a tile ahead of its unpacking and two ahead of their use, and
 // writes them as float16 codes (as in k_attend4_rows) to LDS in the order of the MFMA
-// operands, where V's [dim][slot] cells need no transposing. Two LDS buffers, one barrier a
-// tile. S^T = K Q^T: row 8 a + 4 h + i of a 32-key score tile is block a / 2, slot
+// operands, where V's [dim][slot] cells need no transposing. Two LDS buffers each. S^T = K Q^T: row 8 a + 4 h + i of a 32-key score tile is block a / 2, slot
 // 8 h + 4 (a % 2) + i, so lane half h ends with slots 8 h .. + 8 of both blocks, the k-slots of
 // O^T = V^T P^T. Scales, minima, the reference M and float16 pairs as in k_attend4_rows;
 // in bf16 calls q is one exact float16 and P one float16, half the products.
@@ -677,7 +676,7 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
   constexpr int W = HD / 32;                       // words of a key's row per wave
   constexpr int KB = 64 * HD * 2;                  // bytes of a tile's K (and V) as float16
   extern __shared__ __align__(1024) unsigned char lds[];
-  float* ssc = (float*)(lds + 4 * KB);             // [buffer][K, V][64 keys] (s, m)
+  float* ssc = (float*)(lds + 4 * KB);             // (s, m) of 64 keys, K then V: three buffers, filled two tiles ahead
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hf = lane >> 5, gq = a.n_h / a.n_kv, kvh = blockIdx.x % a.n_kv;
   const int item = blockIdx.x / a.n_kv, PB = 128 / gq;
@@ -714,15 +713,12 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
   // staging: thread (w, lane) brings words W w .. of key `lane`'s row, and the 16 slots of dim `lane` (and
   // + HD / 2) of block w; threads below 128 one scale word (K of keys 0 .. 63, then V)
   const int vb = HD == 128 ? w : threadIdx.x >> 5, vd = HD == 128 ? lane : lane & 31;
-  const bool has_v = HD == 128 || w < 2, has_s = w < 2;
-  unsigned kid, vid;
-  auto ids = [&](int t) {
-    kid = id_of(4 * t + (lane >> 4));
-    vid = id_of(4 * t + min(vb, 3));
-  };
-  unsigned kw[W], sw;
+  const bool has_v = HD == 128 || w < 2;
+  unsigned kid, vid, kw[W], ks;
   u32x4 vw;
-  auto load = [&](int t) {
+  // row of the score tile that key `lane` takes
+  const int krow = 8 * (2 * ((lane >> 4) & 1) + ((lane >> 2) & 1)) + 4 * ((lane >> 3) & 1) + (lane & 3);
+  auto load_k = [&](int t) {                       // the ids that it needs came a tile before
     const unsigned char* cell = pool + kid * stride;
     if constexpr (W == 4) {
       const u32x4 x = *(const u32x4*)(cell + (lane & 15) * (HD / 2) + w * 16);
@@ -731,22 +727,29 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
       const u32x2_t x = *(const u32x2_t*)(cell + (lane & 15) * (HD / 2) + w * 8);
       kw[0] = x[0]; kw[1] = x[1];
     }
-    if (has_s) {
-      sw = *(const unsigned*)(cell + 16 * HD + 64 * w + 4 * (lane & 15));
-      if (64 * t + lane >= kmax) sw = 0;           // whatever lies behind the last key
+    // scale words of key `lane`: K's by wave 0, V's (of the same tile) by wave 1
+    if (w < 2) {
+      ks = *(const unsigned*)(cell + 16 * HD + 64 * w + 4 * (lane & 15));
+      if (64 * t + lane >= kmax) ks = 0;           // whatever lies behind the last key
     }
-    if (has_v) vw = *(const u32x4*)(pool + vid * stride + 8 * HD + vd * 16);
+    kid = id_of(4 * (t + 1) + (lane >> 4));
   };
-  // row of the score tile that key `lane` takes
-  const int krow = 8 * (2 * ((lane >> 4) & 1) + ((lane >> 2) & 1)) + 4 * ((lane >> 3) & 1) + (lane & 3);
-  auto unpack = [&](int t) {
-    unsigned char* kb = lds + (t & 1) * KB;
-    unsigned char* vbuf = lds + 2 * KB + (t & 1) * KB;
+  auto load_v = [&](int t) {
+    if (has_v) vw = *(const u32x4*)(pool + vid * stride + 8 * HD + vd * 16);
+    vid = id_of(4 * (t + 1) + min(vb, 3));
+  };
+  auto unpack_k = [&](int t) __attribute__((always_inline)) {
+    unsigned char* kb = lds + (t & 1) * KB + (((lane >> 5) * DS + (W * w >> 1)) * 64 + krow) * 16;
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      const int x = W * w + j;                     // the word's dims: step x / 2, half x % 2
-      *(u32x4*)(kb + (((lane >> 5) * DS + (x >> 1)) * 64 + (x & 1) * 32 + krow) * 16) = codes_f16(kw[j]);
+    for (int j = 0; j < W; ++j)                    // word W w + j: half j % 2 of step (W w + j) / 2
+      *(u32x4*)(kb + (j >> 1) * 1024 + (j & 1) * 512) = codes_f16(kw[j]);
+    if (w < 2) {
+      const float s = __uint_as_float(ks << 16), m = __uint_as_float(ks & 0xffff0000u);
+      *(float2*)&ssc[((t % 3 * 2 + w) * 64 + lane) * 2] = w == 0 ? make_float2(s * 0x1p20f, m) : make_float2(s, FINE && s == s ? fmaf(s, 8.f, m) : m);
     }
+  };
+  auto unpack_v = [&](int t) __attribute__((always_inline)) {
+    unsigned char* f = lds + 2 * KB + (t & 1) * KB + ((vb * DT + (vd >> 5)) * 64 + (vd & 31)) * 16;
     if (has_v) {
 #pragma unroll
       for (int o = 0; o < 2; ++o) {
@@ -759,17 +762,16 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
           lo = u32x4{(x << 4) & kCodeMask, (x >> 4) & kCodeMask, (y << 4) & kCodeMask, (y >> 4) & kCodeMask};
           hi = u32x4{x & kCodeMask, (x >> 8) & kCodeMask, y & kCodeMask, (y >> 8) & kCodeMask};
         }
-        unsigned char* f = vbuf + ((vb * DT + (vd >> 5)) * 64 + o * 32 + (vd & 31)) * 16;
-        *(u32x4*)f = lo;
-        *(u32x4*)(f + DT / 2 * 1024) = hi;
+        *(u32x4*)(f + o * 512) = lo;
+        *(u32x4*)(f + o * 512 + DT / 2 * 1024) = hi;
       }
     }
-    if (has_s) {
-      const float s = __uint_as_float(sw << 16), m = __uint_as_float(sw & 0xffff0000u);
-      *(float2*)&ssc[((t & 1) * 128 + 64 * w + lane) * 2] =
-          w == 0 ? make_float2(s * 0x1p20f, m) : make_float2(s, FINE && s == s ? fmaf(s, 8.f, m) : m);
-    }
   };
+  const int ta = k0 >> 6, tb = (k1 + 63) >> 6;     // tiles
+  kid = id_of(4 * ta + (lane >> 4));
+  vid = id_of(4 * ta + min(vb, 3));
+  load_k(ta);
+  load_v(ta);
 
   // B operand of the scores: query `slot`, dims 16 s + 8 hf .. + 8 in the order of codes_f16
   u32x4 qh[DS], ql[FINE ? DS : 1];
@@ -807,114 +809,119 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
     Q = add_halves(sum);
   }
 
-  f32x16_t O[DT];
+  f32x16_t O[DT], S, N;                            // the answer, a subtile's scores, the next one's products
 #pragma unroll
   for (int d = 0; d < DT; ++d) O[d] = f32x16_t{};
   float M = -INFINITY, l = 0.f, mv = 0.f;
-  const int ta = k0 >> 6, tb = (k1 + 63) >> 6;     // tiles
   const int first_pos = c.pos0 + min(32 * w, c.nq * gq - 1) / gq;
-  ids(ta);
-  load(ta);
-  ids(ta + 1);
-  unpack(ta);
-  load(ta + 1);
-  ids(ta + 2);
-  __syncthreads();
-  for (int t = ta; t < tb; ++t) {
-    const unsigned char* kb = lds + (t & 1) * KB;
-    const unsigned char* vbuf = lds + 2 * KB + (t & 1) * KB;
-    f32x16_t S[2];
+  auto product = [&](const unsigned char* kf, int s) __attribute__((always_inline)) {
+    const f16x8_t x = __builtin_bit_cast(f16x8_t, *(const u32x4*)(kf + (s * 64 + lane) * 16));
+    N = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, qh[s]), s ? N : f32x16_t{}, 0, 0, 0);
+    if constexpr (FINE) N = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, ql[s]), N, 0, 0, 0);
+  };
+  // Subtile k of tile t: its softmax beside the products of the next subtile (at kf), a
+  // share of each at a time, so that one wave keeps both the matrix cores and the VALU; then P V.
+  auto stage = [&](int t, int k, const unsigned char* kf) __attribute__((always_inline)) {
+    // element e: key 64 t + 32 k + 16 (e / 8) + 8 hf + e % 8
+    const float* kc = ssc + (t % 3 * 128 + 32 * k + 8 * hf) * 2;
+    const float* vc = kc + 128;
+    const bool masked = 64 * t + 32 * k + 31 > first_pos;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      S[k] = f32x16_t{};
-#pragma unroll
-      for (int s = 0; s < DS; ++s) {
-        const f16x8_t x = __builtin_bit_cast(f16x8_t, *(const u32x4*)(kb + ((k * DS + s) * 64 + lane) * 16));
-        S[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, qh[s]), S[k], 0, 0, 0);
-        if constexpr (FINE) S[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, ql[s]), S[k], 0, 0, 0);
-      }
+    for (int e = 0; e < 16; ++e) {
+      const float2 sm = *(const float2*)(kc + (16 * (e >> 3) + (e & 7)) * 2);
+      S[e] = fmaf(sm.x, S[e], sm.y * Q);
     }
-    const bool masked = 64 * t + 63 > first_pos;   // some query of the wave does not see the whole tile
+    if (masked) {
+      const int see = qpos - (64 * t + 32 * k + 8 * hf);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      // element e: key 64 t + 32 k + 16 (e / 8) + 8 hf + e % 8
-      const float* kc = ssc + ((t & 1) * 128 + 32 * k + 8 * hf) * 2;
-      const float* vc = kc + 128;
+      for (int e = 0; e < 16; ++e)
+        if (16 * (e >> 3) + (e & 7) > see) S[e] = -INFINITY;
+    }
+    float pv[16], ts = 0.f, tm = 0.f, pm = 0.f;
+    auto probability = [&](int e, float base) __attribute__((always_inline)) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(S[e], f, -base));
+      const float2 sm = *(const float2*)(vc + (16 * (e >> 3) + (e & 7)) * 2);
+      pv[e] = p * sm.x;
+      ts += p;
+      tm = fmaf(p, sm.y, tm);
+      pm = fmaxf(pm, pv[e]);
+    };
+    const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+      product(kf, s);
+#pragma unroll
+      for (int e = 16 * s / DS; e < 16 * (s + 1) / DS; ++e) probability(e, base);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the reference moves: at the first keys that a query meets, or past 2^13
+    const int fine = __all(pm <= 8192.f && ts < INFINITY) & !__any(M == -INFINITY);
+    if (!fine) {
+      float u = -INFINITY, big = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float2 sm = *(const float2*)(kc + (16 * (e >> 3) + (e & 7)) * 2);
-        S[k][e] = fmaf(sm.x, S[k][e], sm.y * Q);
+        u = fmaxf(u, S[e]);
+        big = fmaxf(big, vc[(16 * (e >> 3) + (e & 7)) * 2]);
       }
-      if (masked) {
+      u = fmaf(max_halves(u), f, fmaxf(__builtin_amdgcn_logf(max_halves(big)), -90.f));
+      u = fmaxf(u - 8.f, M);
+      const float alpha = M == u ? 1.f : __builtin_amdgcn_exp2f(M - u);
+      M = u;
+      l *= alpha;
+      mv *= alpha;
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (64 * t + 32 * k + 16 * (e >> 3) + 8 * hf + (e & 7) > qpos) S[k][e] = -INFINITY;
+      for (int d = 0; d < DT; ++d) O[d] *= alpha;
+      ts = tm = pm = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) probability(e, M == -INFINITY ? 0.f : M);
+    }
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (S[e] == -INFINITY) pv[e] = 0.f;        // also where the unseen row stands for NaN
+    }
+    l += ts;
+    mv += tm;
+    const unsigned char* vf = lds + 2 * KB + (t & 1) * KB + 2 * k * DT * 1024 + lane * 16;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      u32x4 ph, pl;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = 8 * u + 4 * (i >> 1) + (i & 1);
+        ph[i] = pack_f16(pv[e], pv[e + 2]);
+        if constexpr (FINE) {
+          const f16x2_t g = __builtin_bit_cast(f16x2_t, (unsigned)ph[i]);
+          pl[i] = pack_f16(pv[e] - (float)g[0], pv[e + 2] - (float)g[1]);
+        }
       }
-      float pv[16], ts, tm, pm;
-      auto probabilities = [&](float base) {
-        ts = tm = pm = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(S[k][e], f, -base));
-          const float2 sm = *(const float2*)(vc + (16 * (e >> 3) + (e & 7)) * 2);
-          pv[e] = p * sm.x;
-          ts += p;
-          tm = fmaf(p, sm.y, tm);
-          pm = fmaxf(pm, pv[e]);
-        }
-      };
-      const bool first = __any(M == -INFINITY);    // also while a query has not met a key
-      if (!first) probabilities(M);
-      if (first || !__all(pm <= 8192.f && ts < INFINITY)) {
-        float u = -INFINITY, big = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          u = fmaxf(u, S[k][e]);
-          big = fmaxf(big, vc[(16 * (e >> 3) + (e & 7)) * 2]);
-        }
-        u = fmaf(max_halves(u), f, fmaxf(__builtin_amdgcn_logf(max_halves(big)), -90.f));
-        u = fmaxf(u - 8.f, M);
-        const float alpha = M == u ? 1.f : __builtin_amdgcn_exp2f(M - u);
-        M = u;
-        l *= alpha;
-        mv *= alpha;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) O[d] *= alpha;
-        probabilities(M == -INFINITY ? 0.f : M);
-      }
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (S[k][e] == -INFINITY) pv[e] = 0.f;   // also where the unseen row stands for NaN
-        // (its minimum is finite: it adds 0 to the sums)
-      }
-      l += ts;
-      mv += tm;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        u32x4 ph, pl;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 8 * u + 4 * (i >> 1) + (i & 1);
-          ph[i] = pack_f16(pv[e], pv[e + 2]);
-          if constexpr (FINE) {
-            const f16x2_t g = __builtin_bit_cast(f16x2_t, (unsigned)ph[i]);
-            pl[i] = pack_f16(pv[e] - (float)g[0], pv[e + 2] - (float)g[1]);
-          }
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const f16x8_t x = __builtin_bit_cast(f16x8_t, *(const u32x4*)(vbuf + (((2 * k + u) * DT + d) * 64 + lane) * 16));
-          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, ph), O[d], 0, 0, 0);
-          if constexpr (FINE) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, pl), O[d], 0, 0, 0);
-        }
+      for (int d = 0; d < DT; ++d) {
+        const f16x8_t x = __builtin_bit_cast(f16x8_t, *(const u32x4*)(vf + (u * DT + d) * 1024));
+        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, ph), O[d], 0, 0, 0);
+        if constexpr (FINE) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8_t, pl), O[d], 0, 0, 0);
       }
     }
-    if (t + 1 < tb) {
-      unpack(t + 1);
-      load(t + 2);
-      ids(t + 3);
-    }
+    S = N;
+  };
+  unpack_k(ta);
+  unpack_v(ta);
+  load_k(ta + 1);
+  unpack_k(ta + 1);
+  load_k(ta + 2);
+  load_v(ta + 1);
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < DS; ++s) product(lds + (ta & 1) * KB, s);
+  S = N;
+  for (int t = ta; t < tb; ++t) {
+    stage(t, 0, lds + (t & 1) * KB + DS * 1024);
+    __syncthreads();                               // K of tile t has been read
+    unpack_k(t + 2);
+    load_k(t + 3);
+    unpack_v(t + 1);
+    load_v(t + 2);
+    stage(t, 1, lds + ((t + 1) & 1) * KB);       // (behind the last tile: finite codes, never used)
     __syncthreads();
   }
 
@@ -1065,13 +1072,13 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
   if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)nslots * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
   Partial4 part{nullptr, nullptr};
   if (n > 1) part = {(float*)workspace, (float*)((char*)workspace + up256((size_t)n * a.T * a.n_h * a.hd * 4))};
-  const unsigned shm = 4u * 64u * (unsigned)a.hd * 2u + 2048u;
+  const unsigned shm = 4u * 64u * (unsigned)a.hd * 2u + 3u * 1024u;
   const bool vec = a.q_stride % (a.q_bf16 ? 8 : 4) == 0 && (uintptr_t)a.q % 16 == 0;
   static bool attr = false;                // one attribute call per process for the instantiations
   if (!attr) {
     for (const void* f : {(const void*)k_attend4_chunks<64, false, false>, (const void*)k_attend4_chunks<64, false, true>,
                           (const void*)k_attend4_chunks<128, false, false>, (const void*)k_attend4_chunks<128, false, true>}) {
-      const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * 64 * 128 * 2 + 2048);
+      const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * 64 * 128 * 2 + 3 * 1024);
       if (e != hipSuccess) return e;
     }
     attr = true;
