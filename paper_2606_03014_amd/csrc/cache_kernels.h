@@ -40,23 +40,20 @@ __device__ __forceinline__ T over_row(T v, F f) {
 // (bf16 values often do) is a tie here too, and goes to the even code.
 template <int LP>
 __device__ __forceinline__ unsigned quantise(const float x[8], int c[8]) {
+  // NaN goes through these, so one test finds NaN, infinities and ranges past float32
+  auto least = [](float a, float b) { return __builtin_elementwise_minimum(a, b); };
+  auto most = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
   float lo = x[0], hi = x[0];
-  bool fine = true;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-    fine = fine && fabsf(x[i]) < INFINITY;
-  }
-  lo = over_row<LP>(lo, [](float a, float b) { return fminf(a, b); });
-  hi = over_row<LP>(hi, [](float a, float b) { return fmaxf(a, b); });
-  const float ok = over_row<LP>(fine ? 1.f : 0.f, [](float a, float b) { return fminf(a, b); });
+  for (int i = 1; i < 8; ++i) { lo = least(lo, x[i]); hi = most(hi, x[i]); }
+  lo = over_row<LP>(lo, least);
+  hi = over_row<LP>(hi, most);
   uint16_t m = f2bf(lo), s = f2bf((hi - lo) / 15.f);
-  if (ok == 0.f || !(hi - lo < INFINITY) || !(fabsf(bf2f(m)) < INFINITY)) { s = 0x7fc0; m = 0; }
+  if (!(hi - lo < INFINITY) || !(fabsf(bf2f(m)) < INFINITY)) { s = 0x7fc0; m = 0; }
   const float sf = bf2f(s);
   const double md = bf2f(m), inv = sf > 0.f ? 1.0 / (double)sf : 0.0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = sf > 0.f ? (int)fminf(fmaxf(rintf((float)(((double)x[i] - md) * inv)), 0.f), 15.f) : 0;
+  for (int i = 0; i < 8; ++i) c[i] = (int)fminf(fmaxf(rintf((float)(((double)x[i] - md) * inv)), 0.f), 15.f);   // inv = 0: 0, for NaN too
   return (unsigned)s | ((unsigned)m << 16);
 }
 
@@ -98,17 +95,10 @@ __device__ __forceinline__ void store_row(unsigned char* cell, int slot, bool v,
 // Keys of a 4-bit cache are computed in 64 bits: their codes are then
 // those of the float32 value, whatever the order of the norm's sum (one bit of the
 // float32 value can move the row's bf16 minimum, and with it every code).
-template <bool XBF, int KIND, int HD, bool NORM>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, bool aligned) {
-  constexpr int LP = HD / 8;
-  const int H = a.n_h + 2 * a.n_kv;
-  const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LP;
-  const int l = threadIdx.x % LP;
-  const bool live = item < (long long)a.T * H;     // lanes of a row agree; the others' results are dropped
-  const int t = live ? (int)(item / H) : 0, head = live ? (int)(item % H) : 0;
-  const int pos = a.row_pos[t];
-  if (!live || pos < 0 || (a.rope && pos >= a.rope_len)) return;
-  float x[8];
+
+// Lane l's dims of a head of row t.
+template <bool XBF, int HD>
+__device__ __forceinline__ void load_head(const AppendArgs& a, bool aligned, int t, int head, int l, float x[8]) {
   const size_t at = (size_t)t * a.stride + (size_t)head * HD + 4 * l;
   if (XBF) {
     const uint16_t* p = (const uint16_t*)a.x + at;
@@ -137,66 +127,183 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, bool aligned) {
       }
     }
   }
-  const bool is_q = head < a.n_h, is_v = head >= a.n_h + a.n_kv;
-  auto norm_rotate = [&](auto one) {
-    using T = decltype(one);
-    T y[8];
+}
+
+// Lane l's dims of a gain, and its rotation's (cos, sin) at a position.
+template <int HD>
+__device__ __forceinline__ void load_gain(const AppendArgs& a, const ModelPtrs& gains, int t, int l, float g[8]) {
+  const void* p = pick(gains, a.row_model ? a.row_model[t] : 0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (T)x[i];
-    if constexpr (NORM) {
-      const void* g = pick(is_q ? a.q_gain : a.k_gain, a.row_model ? a.row_model[t] : 0);
-      T ss = 0;
+  for (int i = 0; i < 8; ++i) {
+    const int d = 4 * l + (i & 3) + (i >> 2) * (HD / 2);
+    g[i] = a.gain_bf16 ? load_el<true>(p, d) : load_el<false>(p, d);
+  }
+}
+template <int HD>
+__device__ __forceinline__ void load_turn(const AppendArgs& a, int pos, int l, float c[8]) {
+  const float4* cs = (const float4*)(a.rope + (size_t)pos * (HD / 2) + 4 * l);
+  const float4 u = cs[0], w = cs[1];
+  c[0] = u.x; c[1] = u.y; c[2] = u.z; c[3] = u.w;
+  c[4] = w.x; c[5] = w.y; c[6] = w.z; c[7] = w.w;
+}
+
+// Norm (with gain g) and rotation by c, in type T.
+template <typename T, int HD, bool NORM>
+__device__ __forceinline__ void norm_rotate(const AppendArgs& a, const float g[8], const float c[8], float x[8]) {
+  T y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss += y[i] * y[i];
-      ss = over_row<LP>(ss, [](T u, T w) { return u + w; });
-      const T mean = ss / (T)HD + (T)a.eps;
-      const T inv = sizeof(T) == 8 ? (T)(1.0 / sqrt((double)mean)) : (T)rsqrtf((float)mean);
+  for (int i = 0; i < 8; ++i) y[i] = (T)x[i];
+  if constexpr (NORM) {
+    T ss = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = 4 * l + (i & 3) + (i >> 2) * (HD / 2);
-        y[i] *= inv * (T)(a.gain_bf16 ? load_el<true>(g, d) : load_el<false>(g, d));
+    for (int i = 0; i < 8; ++i) ss += y[i] * y[i];
+    ss = over_row<HD / 8>(ss, [](T u, T w) { return u + w; });
+    const T mean = ss / (T)HD + (T)a.eps;
+    const T inv = sizeof(T) == 8 ? (T)(1.0 / sqrt((double)mean)) : (T)rsqrtf((float)mean);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] *= inv * (T)g[i];
+  }
+  if (a.rope) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 8) {
+        const T u = y[i], w = y[i + 4];
+        y[i] = u * c[2 * i] - w * c[2 * i + 1];
+        y[i + 4] = w * c[2 * i] + u * c[2 * i + 1];
+      } else {
+        const float2 r = rotate((float)y[i], (float)y[i + 4], make_float2(c[2 * i], c[2 * i + 1]));
+        y[i] = r.x;
+        y[i + 4] = r.y;
       }
     }
-    if (a.rope) {
-      const float4* cs = (const float4*)(a.rope + (size_t)pos * (HD / 2) + 4 * l);
-      const float4 c01 = cs[0], c23 = cs[1];
-      const float c[8] = {c01.x, c01.y, c01.z, c01.w, c23.x, c23.y, c23.z, c23.w};
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
+}
+
+// A workgroup is a row: its position and block are scalars, its rotation and gains are read once
+// for all heads, and the loads of a thread's (up to three) heads are in flight together.
+template <bool XBF, int KIND, int HD, bool NORM>
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int heads, bool aligned) {
+  constexpr int LP = HD / 8, G = 256 / LP, U = 3;
+  const int t = blockIdx.x, l = threadIdx.x % LP, g = threadIdx.x / LP;
+  float x[U][8], gq[8] = {}, gk[8] = {}, cs[8] = {};
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + u * G < heads) load_head<XBF, HD>(a, aligned, t, h0 + u * G, l, x[u]);
+  };
+  load(g);
+  if constexpr (NORM) {
+    load_gain<HD>(a, a.q_gain, t, l, gq);
+    if (heads > a.n_h) load_gain<HD>(a, a.k_gain, t, l, gk);
+  }
+  const int pos = a.row_pos[t];
+  if (pos < 0 || (a.rope && pos >= a.rope_len)) return;
+  if (a.rope) load_turn<HD>(a, pos, l, cs);
+  const int block = heads > a.n_h ? kv_block(a.place, t, pos) : -1;
+  for (int h0 = g; h0 < heads; h0 += U * G) {
+    if (h0 > g) load(h0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int head = h0 + u * G;
+      if (head >= heads) break;
+      if (head < a.n_h) {
+        norm_rotate<float, HD, NORM>(a, gq, cs, x[u]);
+        const size_t o = ((size_t)t * a.n_h + head) * HD + 4 * l;
+        if (XBF) {
+          *(uint2*)((uint16_t*)a.q + o) = make_uint2(pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3]));
+          *(uint2*)((uint16_t*)a.q + o + HD / 2) = make_uint2(pack_bf16(x[u][4], x[u][5]), pack_bf16(x[u][6], x[u][7]));
+        } else {
+          *(float4*)((float*)a.q + o) = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
+          *(float4*)((float*)a.q + o + HD / 2) = make_float4(x[u][4], x[u][5], x[u][6], x[u][7]);
+        }
+        continue;
+      }
+      const bool is_v = head >= a.n_h + a.n_kv;
+      if (!is_v) {
+        using T = std::conditional_t<KIND == KV_INT4, double, float>;
+        norm_rotate<T, HD, NORM>(a, gk, cs, x[u]);
+      }
+      if (block < 0) continue;
+      const int kh = head - a.n_h - (is_v ? a.n_kv : 0);
+      store_row<HD, KIND>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x[u], l);
+    }
+  }
+}
+
+// The keys and values of rows that follow one another in their sequences, into 4-bit cells:
+// a wave is a run of rows of one block (at most 16) and a KV head, so that a dim of V, whose 16 slots
+// lie side by side, is written in words instead of single bytes (prompts of 18k rows in all, 8 KV
+// heads of 128: 170 us byte by byte, with the queries).
+// A workgroup looks for the runs that begin in its 16 rows; its waves are four heads' keys or values.
+template <bool XBF, int HD, bool NORM>
+__global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool aligned) {
+  constexpr int LP = HD / 8, NR = 64 / LP, NI = 16 / NR;     // rows at a time, slots per group of lanes
+  const int lane = threadIdx.x & 63, l = lane % LP, rg = lane / LP;
+  const int unit = blockIdx.y * 4 + (threadIdx.x >> 6), t0 = blockIdx.x * 16;
+  if (unit >= 2 * a.n_kv) return;
+  const bool is_v = unit >= a.n_kv;
+  const int kh = is_v ? unit - a.n_kv : unit;
+  const int ti = min(t0 + (lane & 15), a.T - 1), tp = max(ti - 1, 0);
+  const int pi = a.row_pos[ti], pp = a.row_pos[tp];
+  const bool follows = ti > 0 && pp >= 0 && pi == pp + 1 && (pi & 15) != 0 && a.place.key[ti] == a.place.key[tp];
+  unsigned long long begin = __ballot(lane < 16 && t0 + lane < a.T && !follows && pi >= 0);
+  while (begin) {
+    const int t1 = t0 + __builtin_ctzll(begin);
+    begin &= begin - 1;
+    const int p1 = a.row_pos[t1], s0 = p1 & 15, key = a.place.key[t1];
+    const int block = kv_block(a.place, t1, p1);
+    if (block < 0) continue;
+    const int tn = min(t1 + (lane & 15), a.T - 1);
+    const bool in = (lane & 15) < 16 - s0 && t1 + (lane & 15) < a.T && a.place.key[tn] == key && a.row_pos[tn] == p1 + (lane & 15);
+    const int n = __builtin_ctz(~((unsigned)__ballot(in) & 0xffffu));
+    unsigned char* cell = kv_cell(a.kv, KV_INT4, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh);
+    float x[NI][8];
+    bool live[NI], whole = true;
+#pragma unroll
+    for (int it = 0; it < NI; ++it) {
+      const int i = rg * NI + it - s0;
+      live[it] = i >= 0 && i < n && !(a.rope && p1 + i >= a.rope_len);
+      whole = whole && live[it];
+      load_head<XBF, HD>(a, aligned, live[it] ? t1 + i : t1, a.n_h + (is_v ? a.n_kv : 0) + kh, l, x[it]);
+    }
+    if (!is_v) {
+#pragma unroll
+      for (int it = 0; it < NI; ++it) {
+        const int slot = rg * NI + it, i = live[it] ? slot - s0 : 0;
+        float g[8], c[8];
+        if constexpr (NORM) load_gain<HD>(a, a.k_gain, t1 + i, l, g);
+        if (a.rope) load_turn<HD>(a, min(p1 + i, a.rope_len - 1), l, c);
+        norm_rotate<double, HD, NORM>(a, g, c, x[it]);
+        if (live[it]) store_row<HD, KV_INT4>(cell, slot, false, x[it], l);
+      }
+      continue;
+    }
+    unsigned word[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int it = 0; it < NI; ++it) {
+      int c[8];
+      const unsigned sc = quantise<LP>(x[it], c);
+      if (live[it] && l == 0) ((unsigned*)(cell + 16 * HD))[16 + rg * NI + it] = sc;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) word[i] |= (unsigned)(c[i] | (c[i + 4] << 4)) << (8 * it);
+    }
+    unsigned char* vp = cell + 8 * HD + 4 * l * 16 + rg * NI;
+    if (whole) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 8) {
-          const T u = y[i], w = y[i + 4];
-          y[i] = u * c[2 * i] - w * c[2 * i + 1];
-          y[i + 4] = w * c[2 * i] + u * c[2 * i + 1];
-        } else {
-          const float2 r = rotate((float)y[i], (float)y[i + 4], make_float2(c[2 * i], c[2 * i + 1]));
-          y[i] = r.x;
-          y[i + 4] = r.y;
-        }
+        if constexpr (NI == 4) *(unsigned*)(vp + i * 16) = word[i];
+        else *(uint16_t*)(vp + i * 16) = (uint16_t)word[i];
       }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
-  };
-  if (is_q) {
-    norm_rotate(0.f);
-    const size_t o = ((size_t)t * a.n_h + head) * HD + 4 * l;
-    if (XBF) {
-      *(uint2*)((uint16_t*)a.q + o) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-      *(uint2*)((uint16_t*)a.q + o + HD / 2) = make_uint2(pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
     } else {
-      *(float4*)((float*)a.q + o) = make_float4(x[0], x[1], x[2], x[3]);
-      *(float4*)((float*)a.q + o + HD / 2) = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+      for (int it = 0; it < NI; ++it)
+        if (live[it])
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vp[i * 16 + it] = (unsigned char)(word[i] >> (8 * it));
     }
-    return;
   }
-  if (!is_v) {
-    if constexpr (KIND == KV_INT4) norm_rotate(0.0);
-    else norm_rotate(0.f);
-  }
-  const int block = kv_block(a.place, t, pos);
-  if (block < 0) return;
-  const int kh = (head - a.n_h) % a.n_kv;
-  store_row<HD, KIND>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x, l);
 }
 
 // ------------------------------------------------- what cached positions hold
@@ -205,11 +312,10 @@ __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, in
                                                  const int* __restrict__ row_pos, KvPlace place, void* __restrict__ kout,
                                                  void* __restrict__ vout) {
   constexpr int LP = HD / 8;
-  const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LP;
-  if (item >= (long long)T * n_kv) return;
-  const int l = threadIdx.x % LP, t = (int)(item / n_kv), kh = (int)(item % n_kv);
+  const int t = blockIdx.x, l = threadIdx.x % LP, kh = blockIdx.y * (256 / LP) + threadIdx.x / LP;
+  if (kh >= n_kv) return;
   const int pos = row_pos[t], block = kv_block(place, t, pos), slot = pos & 15;
-  const size_t o = (size_t)item * HD + 4 * l;
+  const size_t o = ((size_t)t * n_kv + kh) * HD + 4 * l;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     float x[8] = {};
@@ -982,13 +1088,20 @@ __global__ __launch_bounds__(256) void k_attend4_chunks_join(Attend4Args a, int 
 hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a) {
   if (a.T <= 0) return hipSuccess;
   const bool aligned = a.stride % 4 == 0 && a.split_stride % 4 == 0 && (uintptr_t)a.x % (x_bf16 ? 8 : 16) == 0;
-  const long long lanes = (long long)a.T * (a.n_h + 2 * a.n_kv) * (a.hd / 8);
-  const dim3 grid((unsigned)((lanes + 255) / 256)), blk(256);
+  const int all = a.n_h + 2 * a.n_kv, heads = a.runs && kind == KV_INT4 ? a.n_h : all;
+  const dim3 grid(a.T), blk(256);
+  const bool norm = a.q_gain.p[0] != nullptr;
   auto go = [&](auto bf, auto hd, auto k) {
     constexpr bool B = decltype(bf)::value;
     constexpr int D = decltype(hd)::value, K = decltype(k)::value;
-    if (a.q_gain.p[0]) klaunch(k_kv_append<B, K, D, true>, grid, blk, st, a, aligned);
-    else klaunch(k_kv_append<B, K, D, false>, grid, blk, st, a, aligned);
+    if constexpr (K == KV_INT4)
+      if (heads < all) {
+        const dim3 tiles((a.T + 15) / 16, (2 * a.n_kv + 3) / 4);
+        if (norm) klaunch(k_kv_append_runs<B, D, true>, tiles, blk, st, a, aligned);
+        else klaunch(k_kv_append_runs<B, D, false>, tiles, blk, st, a, aligned);
+      }
+    if (norm) klaunch(k_kv_append<B, K, D, true>, grid, blk, st, a, heads, aligned);
+    else klaunch(k_kv_append<B, K, D, false>, grid, blk, st, a, heads, aligned);
     return hipGetLastError();
   };
   auto by_kind = [&](auto bf, auto hd) {
@@ -1007,7 +1120,8 @@ hipError_t launch_kv_read(hipStream_t st, int kind, const void* kv, int layer, i
                           const int* row_pos, const KvPlace& place, void* k, void* v) {
   if (T <= 0) return hipSuccess;
   if (hd != 64 && hd != 128) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(((long long)T * n_kv * (hd / 8) + 255) / 256)), blk(256);
+  const int heads = 2048 / hd;                       // per workgroup
+  const dim3 grid(T, (n_kv + heads - 1) / heads), blk(256);
   auto go = [&](auto kern) { klaunch(kern, grid, blk, st, kv, layer, n_kv, T, row_pos, place, k, v); };
   if (kind == KV_F32) hd == 64 ? go(k_kv_read<KV_F32, 64>) : go(k_kv_read<KV_F32, 128>);
   else if (kind == KV_BF16) hd == 64 ? go(k_kv_read<KV_BF16, 64>) : go(k_kv_read<KV_BF16, 128>);

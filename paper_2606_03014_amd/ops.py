@@ -6,6 +6,7 @@ ValueError before anything is launched; index tensors are read on the GPU (inclu
 of range does). There is no fallback: without the built library or a GPU the calls raise.
 """
 import ctypes as C
+import math
 
 import torch
 
@@ -27,36 +28,46 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+_raw_stream = torch._C._cuda_getCurrentRawStream      # torch.cuda.current_stream() without the Stream object
+_F = {}
 
 
 def _call(name, device, *args):
-    """The library call on `device`."""
-    f = getattr(M.lib(), name)
-    if torch.cuda.current_device() == device.index:
-        code = f(*args)
+    """The library call on `device`, on torch's current stream of it."""
+    f = _F.get(name)
+    if f is None:
+        f = _F[name] = getattr(M.lib(), name)
+    i = device.index
+    if torch._C._cuda_getDevice() == i:
+        code = f(*args, _raw_stream(i))
     else:
         with torch.cuda.device(device):
-            code = f(*args)
+            code = f(*args, _raw_stream(i))
     if code != M.MOA_OK:
         raise M.MoaError(code, name)
 
 
 def _rows(t, name, width, device):
     """A matrix of rows of `width` elements each with a row stride of its own: (type, stride)."""
-    _need(t.device == device and t.dtype in _TYPES, f"{name}: a float32 or bfloat16 tensor on {device}")
-    _need(t.dim() >= 2 and t[0].numel() == width if t.shape[0] else t.dim() >= 2, f"{name}: rows of {width} elements")
+    typ = _TYPES.get(t.dtype)
+    if typ is None or t.device != device:
+        raise ValueError(f"{name}: a float32 or bfloat16 tensor on {device}")
+    n = t.shape[0] if t.dim() >= 2 else -1
+    if n < 0 or t.numel() != n * width or (n == 0 and math.prod(t.shape[1:]) != width):
+        raise ValueError(f"{name}: rows of {width} elements")
+    if t.is_contiguous():
+        return typ, width
     inner = 1
-    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        _need(n == 1 or s == inner, f"{name}: the elements of a row must be contiguous")
-        inner *= n
-    return _TYPES[t.dtype], t.stride(0) if t.shape[0] > 1 else width
+    for k, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if k != 1 and s != inner:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        inner *= k
+    return typ, t.stride(0) if n > 1 else width
 
 
 def _ints(t, name, n, device):
-    _need(t.dtype == torch.int32 and t.device == device and t.dim() == 1 and t.shape[0] == n and
-          (n < 2 or t.stride(0) == 1), f"{name}: {n} contiguous int32 on {device}")
+    if t.dtype != torch.int32 or t.device != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous int32 on {device}")
     return t.data_ptr()
 
 
@@ -80,15 +91,17 @@ class PagedKV:
         _need(pool.is_cuda, "pool: a GPU tensor")
         _need(pool.dtype == torch.uint8 and pool.is_contiguous() and pool.numel() == n.value,
               f"pool: {n.value} contiguous bytes")
-        self.pool, self.device = pool, pool.device
+        self.pool, self.device, self._at = pool, pool.device, pool.data_ptr()
 
     def nbytes(self):
         return self._bytes
 
     def _tables(self, tables):
-        _need(tables.dtype == torch.int32 and tables.device == self.device and tables.dim() == 2 and
-              tables.is_contiguous() and tables.numel() > 0, f"tables: a contiguous int32 matrix on {self.device}")
-        return tables.data_ptr(), tables.shape[0], tables.shape[1]
+        if (tables.dtype != torch.int32 or tables.device != self.device or tables.dim() != 2 or
+                not tables.is_contiguous() or tables.numel() == 0):
+            raise ValueError(f"tables: a contiguous int32 matrix on {self.device}")
+        n, width = tables.shape
+        return tables.data_ptr(), n, width
 
     def append(self, layer, qkv, row_seq, row_pos, tables, rope=None, q_gain=None, k_gain=None, eps=1e-5):
         """Norm (with gains), rotate (with a rope_table()) and cache rows of [queries | keys | values]; returns the
@@ -109,11 +122,11 @@ class PagedKV:
                       g.stride(0) == 1, f"gains: {hd} contiguous float32 or bfloat16 values")
             gain_type = _TYPES[q_gain.dtype]
         q = torch.empty(T, self.n_heads, hd, dtype=qkv.dtype, device=dev)
-        _call("moa_kv_append", dev, self._ref, self.pool.data_ptr(), layer, qkv.data_ptr(), typ, stride, T,
+        _call("moa_kv_append", dev, self._ref, self._at, layer, qkv.data_ptr(), typ, stride, T,
               _ints(row_seq, "row_seq", T, dev), _ints(row_pos, "row_pos", T, dev), tab, n_seqs, table_len,
               rope.data_ptr() if rope is not None else None, rope_len,
               q_gain.data_ptr() if q_gain is not None else None, k_gain.data_ptr() if k_gain is not None else None,
-              gain_type, eps, q.data_ptr(), _stream(dev))
+              gain_type, eps, q.data_ptr())
         return q
 
     def read(self, layer, row_seq, row_pos, tables):
@@ -124,8 +137,8 @@ class PagedKV:
         dt = torch.float32 if self.kind == "f32" else torch.bfloat16
         k = torch.empty(T, self.n_kv_heads, self.head_dim, dtype=dt, device=dev)
         v = torch.empty_like(k)
-        _call("moa_kv_read", dev, self._ref, self.pool.data_ptr(), layer, T, _ints(row_seq, "row_seq", T, dev),
-              _ints(row_pos, "row_pos", T, dev), tab, n_seqs, table_len, k.data_ptr(), v.data_ptr(), _stream(dev))
+        _call("moa_kv_read", dev, self._ref, self._at, layer, T, _ints(row_seq, "row_seq", T, dev),
+              _ints(row_pos, "row_pos", T, dev), tab, n_seqs, table_len, k.data_ptr(), v.data_ptr())
         return k, v
 
     def _out(self, out, q):
@@ -138,7 +151,8 @@ class PagedKV:
     def _workspace(self, name, *args):
         n = C.c_size_t()
         M.check(getattr(M.lib(), name)(self._ref, *args, C.byref(n)), name)
-        return torch.empty(n.value, dtype=torch.uint8, device=self.device) if n.value else None, n.value
+        n = n.value
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None, n
 
     def attend(self, layer, q, row_seq, row_ctx, tables, max_ctx, scale=None, out=None):
         """Decode rows over an int4 pool: row r of q ([rows, n_heads, head_dim]) sees the first row_ctx[r] positions
@@ -149,10 +163,9 @@ class PagedKV:
         tab, n_seqs, table_len = self._tables(tables)
         out = self._out(out, q)
         ws, n = self._workspace("moa_kv_attend_bytes", T, max_ctx)
-        _call("moa_kv_attend", dev, self._ref, self.pool.data_ptr(), layer, q.data_ptr(), typ, stride, T,
+        _call("moa_kv_attend", dev, self._ref, self._at, layer, q.data_ptr(), typ, stride, T,
               _ints(row_seq, "row_seq", T, dev), _ints(row_ctx, "row_ctx", T, dev), tab, n_seqs, table_len, max_ctx,
-              self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr() if n else None, n,
-              _stream(dev))
+              self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr() if n else None, n)
         return out
 
     def attend_chunks(self, layer, q, chunk_start, chunk_ctx, tables, max_ctx, scale=None, out=None):
@@ -164,10 +177,10 @@ class PagedKV:
         tab, n, table_len = self._tables(tables)
         out = self._out(out, q)
         ws, nb = self._workspace("moa_kv_attend_chunks_bytes", T, n, max_ctx)
-        _call("moa_kv_attend_chunks", dev, self._ref, self.pool.data_ptr(), layer, q.data_ptr(), typ, stride, T,
+        _call("moa_kv_attend_chunks", dev, self._ref, self._at, layer, q.data_ptr(), typ, stride, T,
               _ints(chunk_start, "chunk_start", n + 1, dev), _ints(chunk_ctx, "chunk_ctx", n, dev), tab, n, table_len,
               max_ctx, self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
-              ws.data_ptr() if nb else None, nb, _stream(dev))
+              ws.data_ptr() if nb else None, nb)
         return out
 
 
@@ -179,13 +192,15 @@ def score_tokens(logits, tokens, top_k=0):
     typ, stride = _rows(logits, "logits", V, dev)
     _need(V > 0 and 0 <= top_k <= min(V, M.MOA_MAX_TOP), f"top_k: 0 to {M.MOA_MAX_TOP}, at most the vocabulary")
     tok = _ints(tokens, "tokens", R, dev)
-    both = torch.empty(2, R, dtype=torch.float32, device=dev)
+    lp = torch.empty(R, dtype=torch.float32, device=dev)
+    entropy = torch.empty_like(lp)
     ids = torch.empty(R, top_k, dtype=torch.int32, device=dev)
     lps = torch.empty(R, top_k, dtype=torch.float32, device=dev)
     n = C.c_size_t()
     M.check(M.lib().moa_score_tokens_bytes(R, V, top_k, C.byref(n)), "moa_score_tokens_bytes")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
-    _call("moa_score_tokens", dev, logits.data_ptr(), typ, stride, R, V, tok, both[0].data_ptr(), both[1].data_ptr(),
-          top_k, ids.data_ptr() if top_k else None, lps.data_ptr() if top_k else None,
-          ws.data_ptr() if n.value else None, n.value, _stream(dev))
-    return both[0], both[1], ids, lps
+    n = n.value
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _call("moa_score_tokens", dev, logits.data_ptr(), typ, stride, R, V, tok, lp.data_ptr(), entropy.data_ptr(), top_k,
+          ids.data_ptr() if top_k else None, lps.data_ptr() if top_k else None,
+          ws.data_ptr() if n else None, n)
+    return lp, entropy, ids, lps
