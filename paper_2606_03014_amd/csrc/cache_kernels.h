@@ -23,29 +23,30 @@ __device__ __forceinline__ double dpp(double v) {
   const unsigned hi = (unsigned)__builtin_amdgcn_mov_dpp((int)(unsigned)(u >> 32), CTRL, 0xF, 0xF, true);
   return __builtin_bit_cast(double, ((unsigned long long)hi << 32) | lo);
 }
-// Combine over the LP lanes (8 or 16) that hold one row of a head; all get the result.
+// Combine over the LP lanes (4, 8 or 16) that hold one row of a head; all get the result.
 template <int LP, typename T, typename F>
 __device__ __forceinline__ T over_row(T v, F f) {
   v = f(v, dpp<0xB1>(v));
   v = f(v, dpp<0x4E>(v));
-  v = f(v, dpp<0x141>(v));
+  if constexpr (LP >= 8) v = f(v, dpp<0x141>(v));
   if constexpr (LP == 16) v = f(v, dpp<0x128>(v));
   return v;
 }
 
-// One 4-bit row from LP = hd / 8 lanes, lane l holding dims 4 l .. 4 l + 3 and the
-// same + hd / 2: its scale word and the lane's eight codes.
+// One 4-bit row from hd / N lanes, lane l holding dims N / 2 l .. + N / 2 and the
+// same + hd / 2: its scale word and the lane's N codes.
 // The quotient is formed in 64 bits from the exact difference and rounded to 24
 // before the rounding to a code, so a quotient that lies on the border of two codes
 // (bf16 values often do) is a tie here too, and goes to the even code.
-template <int LP>
-__device__ __forceinline__ unsigned quantise(const float x[8], int c[8]) {
+template <int HD, int N>
+__device__ __forceinline__ unsigned quantise(const float x[N], int c[N]) {
+  constexpr int LP = HD / N;
   // NaN goes through these, so one test finds NaN, infinities and ranges past float32
   auto least = [](float a, float b) { return __builtin_elementwise_minimum(a, b); };
   auto most = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
   float lo = x[0], hi = x[0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) { lo = least(lo, x[i]); hi = most(hi, x[i]); }
+  for (int i = 1; i < N; ++i) { lo = least(lo, x[i]); hi = most(hi, x[i]); }
   lo = over_row<LP>(lo, least);
   hi = over_row<LP>(hi, most);
   uint16_t m = f2bf(lo), s = f2bf((hi - lo) / 15.f);
@@ -53,7 +54,7 @@ __device__ __forceinline__ unsigned quantise(const float x[8], int c[8]) {
   const float sf = bf2f(s);
   const double md = bf2f(m), inv = sf > 0.f ? 1.0 / (double)sf : 0.0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = (int)fminf(fmaxf(rintf((float)(((double)x[i] - md) * inv)), 0.f), 15.f);   // inv = 0: 0, for NaN too
+  for (int i = 0; i < N; ++i) c[i] = (int)fminf(fmaxf(rintf((float)(((double)x[i] - md) * inv)), 0.f), 15.f);   // inv = 0: 0, for NaN too
   return (unsigned)s | ((unsigned)m << 16);
 }
 
@@ -62,174 +63,193 @@ __device__ __forceinline__ float load_el(const void* p, size_t i) {
   return BF ? bf2f(((const uint16_t*)p)[i]) : ((const float*)p)[i];
 }
 
-// Store a row held as for quantise() (lane l of LP) as K (v = false) or V of a cell's slot.
-template <int HD, int KIND>
-__device__ __forceinline__ void store_row(unsigned char* cell, int slot, bool v, const float x[8], int l) {
-  if constexpr (KIND == KV_INT4) {
-    int c[8];
-    const unsigned sc = quantise<HD / 8>(x, c);
-    if (v) {
-      unsigned char* p = cell + 8 * HD + 4 * l * 16 + slot;
+// N consecutive elements as float32; vec: 16-byte loads (8 for four bf16) may be used.
+template <int N>
+__device__ __forceinline__ void load_run(const void* p, size_t at, bool bf16, bool vec, float* v) {
+  if (vec && bf16 && N % 8 != 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i * 16] = (unsigned char)(c[i] | (c[i + 4] << 4));
+    for (int i = 0; i < N; i += 4) {
+      const u32x2_t x = *(const u32x2_t*)((const uint16_t*)p + at + i);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        v[i + 2 * k] = __uint_as_float(x[k] << 16);
+        v[i + 2 * k + 1] = __uint_as_float(x[k] & 0xffff0000u);
+      }
+    }
+  } else if (vec && bf16) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      const u32x4 x = *(const u32x4*)((const uint16_t*)p + at + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[i + 2 * k] = __uint_as_float(x[k] << 16);
+        v[i + 2 * k + 1] = __uint_as_float(x[k] & 0xffff0000u);
+      }
+    }
+  } else if (vec) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const f32x4_t x = *(const f32x4_t*)((const float*)p + at + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[i + k] = x[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = bf16 ? load_el<true>(p, at + i) : load_el<false>(p, at + i);
+  }
+}
+
+// Four consecutive values as float32 or bf16.
+__device__ __forceinline__ void store4(void* p, bool bf16, size_t at, const float* x) {
+  if (bf16) *(uint2*)((uint16_t*)p + at) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+  else *(float4*)((float*)p + at) = make_float4(x[0], x[1], x[2], x[3]);
+}
+// Lane l's part of a row of hd values, both halves.
+template <int HD, int N>
+__device__ __forceinline__ void store_part(void* p, bool bf16, size_t at, int l, const float x[N]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const size_t o = at + h * (HD / 2) + N / 2 * l;
+    const float* y = x + h * (N / 2);
+    if constexpr (N == 16) {
+      if (bf16) {
+        *(u32x4*)((uint16_t*)p + o) = u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+        continue;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N / 2; i += 4) store4(p, bf16, o + i, y + i);
+  }
+}
+
+// Store a row held as for quantise() (lane l) as K (v = false) or V of a cell's slot.
+template <int HD, int KIND, int N>
+__device__ __forceinline__ void store_row(unsigned char* cell, int slot, bool v, const float x[N], int l) {
+  if constexpr (KIND == KV_INT4) {
+    int c[N];
+    const unsigned sc = quantise<HD, N>(x, c);
+    if (v) {
+      unsigned char* p = cell + 8 * HD + N / 2 * l * 16 + slot;
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) p[i * 16] = (unsigned char)(c[i] | (c[i + N / 2] << 4));
     } else {
-      uint16_t* p = (uint16_t*)(cell + slot * (HD / 2) + 2 * l);
-      p[0] = (uint16_t)(c[0] | (c[1] << 4) | (c[2] << 8) | (c[3] << 12));
-      p[HD / 8] = (uint16_t)(c[4] | (c[5] << 4) | (c[6] << 8) | (c[7] << 12));
+      unsigned char* p = cell + slot * (HD / 2) + N / 4 * l;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        unsigned word = 0;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) word |= (unsigned)c[h * (N / 2) + i] << (4 * i);
+        if constexpr (N == 16) *(unsigned*)(p + h * (HD / 4)) = word;
+        else *(uint16_t*)(p + h * (HD / 4)) = (uint16_t)word;
+      }
     }
     if (l == 0) ((unsigned*)(cell + 16 * HD))[(v ? 16 : 0) + slot] = sc;
-  } else if constexpr (KIND == KV_BF16) {
-    uint16_t* p = (uint16_t*)cell + ((v ? kBlock : 0) + slot) * HD + 4 * l;
-    *(uint2*)p = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-    *(uint2*)(p + HD / 2) = make_uint2(pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
   } else {
-    float* p = (float*)cell + ((v ? kBlock : 0) + slot) * HD + 4 * l;
-    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-    *(float4*)(p + HD / 2) = make_float4(x[4], x[5], x[6], x[7]);
+    store_part<HD, N>(cell, KIND == KV_BF16, (size_t)((v ? kBlock : 0) + slot) * HD, l, x);
   }
 }
 
 // ------------------------------ per-head norms, rotation and append in one pass
-// hd / 8 lanes hold one head of one row, each both halves of four rotation pairs, so
-// the norm's sum, the row's range and its codes stay within a row of 16 lanes.
+// hd / N lanes hold one head of one row, each both halves of N / 2 rotation pairs, so
+// the norm's sum, the row's range and its codes stay within a row of 16 lanes; N = 8
+// values a lane in float32 and 16 in bf16 are 16-byte loads.
 // Keys of a 4-bit cache are computed in 64 bits: their codes are then
 // those of the float32 value, whatever the order of the norm's sum (one bit of the
 // float32 value can move the row's bf16 minimum, and with it every code).
 
 // Lane l's dims of a head of row t.
-template <bool XBF, int HD>
-__device__ __forceinline__ void load_head(const AppendArgs& a, bool aligned, int t, int head, int l, float x[8]) {
-  const size_t at = (size_t)t * a.stride + (size_t)head * HD + 4 * l;
+template <bool XBF, int HD, int N>
+__device__ __forceinline__ void load_head(const AppendArgs& a, bool aligned, int t, int head, int l, float x[N]) {
+  const size_t at = (size_t)t * a.stride + (size_t)head * HD + N / 2 * l;
   if (XBF) {
-    const uint16_t* p = (const uint16_t*)a.x + at;
-    if (aligned) {
-      const uint2 u = *(const uint2*)p, w = *(const uint2*)(p + HD / 2);
-      x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
-      x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
-      x[4] = __uint_as_float(w.x << 16); x[5] = __uint_as_float(w.x & 0xffff0000u);
-      x[6] = __uint_as_float(w.y << 16); x[7] = __uint_as_float(w.y & 0xffff0000u);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = bf2f(p[(i & 3) + (i >> 2) * (HD / 2)]);
-    }
+    load_run<N / 2>(a.x, at, true, aligned, x);
+    load_run<N / 2>(a.x, at + HD / 2, true, aligned, x + N / 2);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    for (int i = 0; i < N; ++i) x[i] = 0.f;
     for (int s = 0; s < a.nsplit; ++s) {
-      const float* p = (const float*)a.x + (size_t)s * a.split_stride + at;
-      if (aligned) {
-        const float4 u = *(const float4*)p, w = *(const float4*)(p + HD / 2);
-        x[0] += u.x; x[1] += u.y; x[2] += u.z; x[3] += u.w;
-        x[4] += w.x; x[5] += w.y; x[6] += w.z; x[7] += w.w;
-      } else {
+      float y[N];
+      load_run<N / 2>(a.x, at + (size_t)s * a.split_stride, false, aligned, y);
+      load_run<N / 2>(a.x, at + (size_t)s * a.split_stride + HD / 2, false, aligned, y + N / 2);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] += p[(i & 3) + (i >> 2) * (HD / 2)];
-      }
+      for (int i = 0; i < N; ++i) x[i] += y[i];
     }
   }
 }
 
 // Lane l's dims of a gain, and its rotation's (cos, sin) at a position.
-template <int HD>
-__device__ __forceinline__ void load_gain(const AppendArgs& a, const ModelPtrs& gains, int t, int l, float g[8]) {
+template <int HD, int N>
+__device__ __forceinline__ void load_gain(const AppendArgs& a, const ModelPtrs& gains, int t, int l, float g[N]) {
   const void* p = pick(gains, a.row_model ? a.row_model[t] : 0);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int d = 4 * l + (i & 3) + (i >> 2) * (HD / 2);
-    g[i] = a.gain_bf16 ? load_el<true>(p, d) : load_el<false>(p, d);
-  }
+  load_run<N / 2>(p, N / 2 * l, a.gain_bf16, a.gain_vec, g);
+  load_run<N / 2>(p, N / 2 * l + HD / 2, a.gain_bf16, a.gain_vec, g + N / 2);
 }
-template <int HD>
-__device__ __forceinline__ void load_turn(const AppendArgs& a, int pos, int l, float c[8]) {
-  const float4* cs = (const float4*)(a.rope + (size_t)pos * (HD / 2) + 4 * l);
-  const float4 u = cs[0], w = cs[1];
-  c[0] = u.x; c[1] = u.y; c[2] = u.z; c[3] = u.w;
-  c[4] = w.x; c[5] = w.y; c[6] = w.z; c[7] = w.w;
+template <int HD, int N>
+__device__ __forceinline__ void load_turn(const AppendArgs& a, int pos, int l, float c[N]) {
+  load_run<N>(a.rope, ((size_t)pos * (HD / 2) + N / 2 * l) * 2, false, true, c);
 }
 
 // Norm (with gain g) and rotation by c, in type T.
-template <typename T, int HD, bool NORM>
-__device__ __forceinline__ void norm_rotate(const AppendArgs& a, const float g[8], const float c[8], float x[8]) {
-  T y[8];
+template <typename T, int HD, int N, bool NORM>
+__device__ __forceinline__ void norm_rotate(const AppendArgs& a, const float g[N], const float c[N], float x[N]) {
+  constexpr int H = N / 2;
+  T y[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = (T)x[i];
+  for (int i = 0; i < N; ++i) y[i] = (T)x[i];
   if constexpr (NORM) {
     T ss = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss += y[i] * y[i];
-    ss = over_row<HD / 8>(ss, [](T u, T w) { return u + w; });
+    for (int i = 0; i < N; ++i) ss += y[i] * y[i];
+    ss = over_row<HD / N>(ss, [](T u, T w) { return u + w; });
     const T mean = ss / (T)HD + (T)a.eps;
     const T inv = sizeof(T) == 8 ? (T)(1.0 / sqrt((double)mean)) : (T)rsqrtf((float)mean);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] *= inv * (T)g[i];
+    for (int i = 0; i < N; ++i) y[i] *= inv * (T)g[i];
   }
   if (a.rope) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < H; ++i) {
       if constexpr (sizeof(T) == 8) {
-        const T u = y[i], w = y[i + 4];
+        const T u = y[i], w = y[i + H];
         y[i] = u * c[2 * i] - w * c[2 * i + 1];
-        y[i + 4] = w * c[2 * i] + u * c[2 * i + 1];
+        y[i + H] = w * c[2 * i] + u * c[2 * i + 1];
       } else {
-        const float2 r = rotate((float)y[i], (float)y[i + 4], make_float2(c[2 * i], c[2 * i + 1]));
+        const float2 r = rotate((float)y[i], (float)y[i + H], make_float2(c[2 * i], c[2 * i + 1]));
         y[i] = r.x;
-        y[i + 4] = r.y;
+        y[i + H] = r.y;
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
+  for (int i = 0; i < N; ++i) x[i] = (float)y[i];
 }
 
-// A workgroup is a row: its position and block are scalars, its rotation and gains are read once
-// for all heads, and the loads of a thread's (up to three) heads are in flight together.
+// A workgroup is one row's next 256 / LP heads of the first `heads`: its position and block are scalars.
 template <bool XBF, int KIND, int HD, bool NORM>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int heads, bool aligned) {
-  constexpr int LP = HD / 8, G = 256 / LP, U = 3;
-  const int t = blockIdx.x, l = threadIdx.x % LP, g = threadIdx.x / LP;
-  float x[U][8], gq[8] = {}, gk[8] = {}, cs[8] = {};
-  auto load = [&](int h0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (h0 + u * G < heads) load_head<XBF, HD>(a, aligned, t, h0 + u * G, l, x[u]);
-  };
-  load(g);
-  if constexpr (NORM) {
-    load_gain<HD>(a, a.q_gain, t, l, gq);
-    if (heads > a.n_h) load_gain<HD>(a, a.k_gain, t, l, gk);
-  }
+  constexpr int N = XBF ? 16 : 8, LP = HD / N;
+  const int t = blockIdx.x, l = threadIdx.x % LP, head = blockIdx.y * (256 / LP) + threadIdx.x / LP;
+  if (head >= heads) return;
+  float x[N], g[N], c[N];
+  load_head<XBF, HD, N>(a, aligned, t, head, l, x);
+  const bool is_q = head < a.n_h, is_v = head >= a.n_h + a.n_kv;
+  if (NORM && !is_v) load_gain<HD, N>(a, is_q ? a.q_gain : a.k_gain, t, l, g);
   const int pos = a.row_pos[t];
   if (pos < 0 || (a.rope && pos >= a.rope_len)) return;
-  if (a.rope) load_turn<HD>(a, pos, l, cs);
-  const int block = heads > a.n_h ? kv_block(a.place, t, pos) : -1;
-  for (int h0 = g; h0 < heads; h0 += U * G) {
-    if (h0 > g) load(h0);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int head = h0 + u * G;
-      if (head >= heads) break;
-      if (head < a.n_h) {
-        norm_rotate<float, HD, NORM>(a, gq, cs, x[u]);
-        const size_t o = ((size_t)t * a.n_h + head) * HD + 4 * l;
-        if (XBF) {
-          *(uint2*)((uint16_t*)a.q + o) = make_uint2(pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3]));
-          *(uint2*)((uint16_t*)a.q + o + HD / 2) = make_uint2(pack_bf16(x[u][4], x[u][5]), pack_bf16(x[u][6], x[u][7]));
-        } else {
-          *(float4*)((float*)a.q + o) = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
-          *(float4*)((float*)a.q + o + HD / 2) = make_float4(x[u][4], x[u][5], x[u][6], x[u][7]);
-        }
-        continue;
-      }
-      const bool is_v = head >= a.n_h + a.n_kv;
-      if (!is_v) {
-        using T = std::conditional_t<KIND == KV_INT4, double, float>;
-        norm_rotate<T, HD, NORM>(a, gk, cs, x[u]);
-      }
-      if (block < 0) continue;
-      const int kh = head - a.n_h - (is_v ? a.n_kv : 0);
-      store_row<HD, KIND>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x[u], l);
-    }
+  if (a.rope && !is_v) load_turn<HD, N>(a, pos, l, c);
+  if (is_q) {
+    norm_rotate<float, HD, N, NORM>(a, g, c, x);
+    store_part<HD, N>(a.q, XBF, ((size_t)t * a.n_h + head) * HD, l, x);
+    return;
   }
+  if (!is_v) {
+    using T = std::conditional_t<KIND == KV_INT4, double, float>;
+    norm_rotate<T, HD, N, NORM>(a, g, c, x);
+  }
+  const int block = kv_block(a.place, t, pos);
+  if (block < 0) return;
+  const int kh = head - a.n_h - (is_v ? a.n_kv : 0);
+  store_row<HD, KIND, N>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x, l);
 }
 
 // The keys and values of rows that follow one another in their sequences, into 4-bit cells:
@@ -266,17 +286,17 @@ __global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool align
       const int i = rg * NI + it - s0;
       live[it] = i >= 0 && i < n && !(a.rope && p1 + i >= a.rope_len);
       whole = whole && live[it];
-      load_head<XBF, HD>(a, aligned, live[it] ? t1 + i : t1, a.n_h + (is_v ? a.n_kv : 0) + kh, l, x[it]);
+      load_head<XBF, HD, 8>(a, aligned, live[it] ? t1 + i : t1, a.n_h + (is_v ? a.n_kv : 0) + kh, l, x[it]);
     }
     if (!is_v) {
 #pragma unroll
       for (int it = 0; it < NI; ++it) {
         const int slot = rg * NI + it, i = live[it] ? slot - s0 : 0;
         float g[8], c[8];
-        if constexpr (NORM) load_gain<HD>(a, a.k_gain, t1 + i, l, g);
-        if (a.rope) load_turn<HD>(a, min(p1 + i, a.rope_len - 1), l, c);
-        norm_rotate<double, HD, NORM>(a, g, c, x[it]);
-        if (live[it]) store_row<HD, KV_INT4>(cell, slot, false, x[it], l);
+        if constexpr (NORM) load_gain<HD, 8>(a, a.k_gain, t1 + i, l, g);
+        if (a.rope) load_turn<HD, 8>(a, min(p1 + i, a.rope_len - 1), l, c);
+        norm_rotate<double, HD, 8, NORM>(a, g, c, x[it]);
+        if (live[it]) store_row<HD, KV_INT4, 8>(cell, slot, false, x[it], l);
       }
       continue;
     }
@@ -284,7 +304,7 @@ __global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool align
 #pragma unroll
     for (int it = 0; it < NI; ++it) {
       int c[8];
-      const unsigned sc = quantise<LP>(x[it], c);
+      const unsigned sc = quantise<HD, 8>(x[it], c);
       if (live[it] && l == 0) ((unsigned*)(cell + 16 * HD))[16 + rg * NI + it] = sc;
 #pragma unroll
       for (int i = 0; i < 4; ++i) word[i] |= (unsigned)(c[i] | (c[i + 4] << 4)) << (8 * it);
@@ -315,7 +335,7 @@ __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, in
   const int t = blockIdx.x, l = threadIdx.x % LP, kh = blockIdx.y * (256 / LP) + threadIdx.x / LP;
   if (kh >= n_kv) return;
   const int pos = row_pos[t], block = kv_block(place, t, pos), slot = pos & 15;
-  const size_t o = ((size_t)t * n_kv + kh) * HD + 4 * l;
+  const size_t o = ((size_t)t * n_kv + kh) * HD;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     float x[8] = {};
@@ -342,14 +362,7 @@ __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, in
           x[i] = load_el<KIND == KV_BF16>(cell, (v * kBlock + slot) * HD + 4 * l + (i & 3) + (i >> 2) * (HD / 2));
       }
     }
-    void* out = v ? vout : kout;
-    if constexpr (KIND == KV_F32) {
-      *(float4*)((float*)out + o) = make_float4(x[0], x[1], x[2], x[3]);
-      *(float4*)((float*)out + o + HD / 2) = make_float4(x[4], x[5], x[6], x[7]);
-    } else {
-      *(uint2*)((uint16_t*)out + o) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-      *(uint2*)((uint16_t*)out + o + HD / 2) = make_uint2(pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-    }
+    store_part<HD, 8>(v ? vout : kout, KIND != KV_F32, o, l, x);
   }
 }
 
@@ -410,32 +423,6 @@ __device__ __forceinline__ u32x4 codes_mixed(unsigned w) {
 }
 __device__ __forceinline__ u32x4 codes_f16(unsigned w) {
   return u32x4{(w << 4) & kCodeMask, w & kCodeMask, (w >> 4) & kCodeMask, (w >> 8) & kCodeMask};
-}
-
-// n consecutive elements as float32; vec: 16-byte loads may be used.
-template <int N>
-__device__ __forceinline__ void load_run(const void* p, size_t at, bool bf16, bool vec, float* v) {
-  if (vec && bf16) {
-#pragma unroll
-    for (int i = 0; i < N; i += 8) {
-      const u32x4 x = *(const u32x4*)((const uint16_t*)p + at + i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[i + 2 * k] = __uint_as_float(x[k] << 16);
-        v[i + 2 * k + 1] = __uint_as_float(x[k] & 0xffff0000u);
-      }
-    }
-  } else if (vec) {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const f32x4_t x = *(const f32x4_t*)((const float*)p + at + i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[i + k] = x[k];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = bf16 ? load_el<true>(p, at + i) : load_el<false>(p, at + i);
-  }
 }
 
 template <int HD, bool ITEMS, bool FINE>
@@ -1085,11 +1072,17 @@ __global__ __launch_bounds__(256) void k_attend4_chunks_join(Attend4Args a, int 
 
 // =============================================================== launchers
 
-hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a) {
-  if (a.T <= 0) return hipSuccess;
-  const bool aligned = a.stride % 4 == 0 && a.split_stride % 4 == 0 && (uintptr_t)a.x % (x_bf16 ? 8 : 16) == 0;
+hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& args) {
+  if (args.T <= 0) return hipSuccess;
+  AppendArgs a = args;
+  a.gain_vec = true;
+  for (int i = 0; i < kMaxModels; ++i)
+    a.gain_vec = a.gain_vec && (uintptr_t)a.q_gain.p[i] % 16 == 0 && (uintptr_t)a.k_gain.p[i] % 16 == 0;
+  const size_t el = x_bf16 ? 8 : 4;                  // elements per 16 bytes
+  const bool aligned = a.stride % el == 0 && a.split_stride % el == 0 && (uintptr_t)a.x % 16 == 0;
   const int all = a.n_h + 2 * a.n_kv, heads = a.runs && kind == KV_INT4 ? a.n_h : all;
-  const dim3 grid(a.T), blk(256);
+  const int wg = 256 * (x_bf16 ? 16 : 8) / a.hd;      // heads per workgroup
+  const dim3 grid(a.T, (heads + wg - 1) / wg), blk(256);
   const bool norm = a.q_gain.p[0] != nullptr;
   auto go = [&](auto bf, auto hd, auto k) {
     constexpr bool B = decltype(bf)::value;

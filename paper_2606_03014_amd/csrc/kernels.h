@@ -207,7 +207,7 @@ struct AppendArgs {
   int rope_len;
   ModelPtrs q_gain, k_gain;// per model, [hd]; entry 0 null: no norm
   const int* row_model;    // null: model 0
-  bool gain_bf16;
+  bool gain_bf16, gain_vec;// gain_vec: set by the launcher (16-byte aligned gains)
   float eps;
   void* q;                 // [T][n_h][hd]
   void* kv;
