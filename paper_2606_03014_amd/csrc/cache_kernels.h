@@ -7,9 +7,8 @@ __device__ __forceinline__ unsigned char* kv_cell(const void* kv, int kind, int 
                                                   int n_kv, int head) {
   return (unsigned char*)kv + (((size_t)layer * num_blocks + block) * n_kv + head) * kv_cell_bytes(kind, hd);
 }
-// The block of a row's position, -1 if anything is out of range.
-__device__ __forceinline__ int kv_block(const KvPlace& p, int row, int pos) {
-  const int key = p.key[row];
+// The block of a position of sequence `key`, -1 if anything is out of range.
+__device__ __forceinline__ int kv_block(const KvPlace& p, int key, int pos) {
   if ((unsigned)key >= (unsigned)p.n_keys || pos < 0 || (pos >> 4) >= p.table_len) return -1;
   const int b = p.tables[(size_t)key * p.mul + (pos >> 4)];
   return (unsigned)b < (unsigned)p.num_blocks ? b : -1;
@@ -49,13 +48,15 @@ __device__ __forceinline__ unsigned quantise(const float x[N], int c[N]) {
   for (int i = 1; i < N; ++i) { lo = least(lo, x[i]); hi = most(hi, x[i]); }
   lo = over_row<LP>(lo, least);
   hi = over_row<LP>(hi, most);
-  uint16_t m = f2bf(lo), s = f2bf((hi - lo) / 15.f);
-  if (!(hi - lo < INFINITY) || !(fabsf(bf2f(m)) < INFINITY)) { s = 0x7fc0; m = 0; }
-  const float sf = bf2f(s);
-  const double md = bf2f(m), inv = sf > 0.f ? 1.0 / (double)sf : 0.0;
+  unsigned word = pack_bf16((hi - lo) / 15.f, lo);
+  if (!(hi - lo < INFINITY) || !(fabsf(__uint_as_float(word & 0xffff0000u)) < INFINITY)) word = 0x7fc0u;
+  const float sf = __uint_as_float(word << 16);
+  // 2^-40 of the reciprocal is enough: the quotient is rounded to 24 bits
+  const double md = __uint_as_float(word & 0xffff0000u), sd = sf > 0.f ? (double)sf : 1.0, r = __builtin_amdgcn_rcp(sd);
+  const double inv = sf > 0.f ? r * (2.0 - sd * r) : 0.0;
 #pragma unroll
   for (int i = 0; i < N; ++i) c[i] = (int)fminf(fmaxf(rintf((float)(((double)x[i] - md) * inv)), 0.f), 15.f);   // inv = 0: 0, for NaN too
-  return (unsigned)s | ((unsigned)m << 16);
+  return word;
 }
 
 template <bool BF>
@@ -202,7 +203,14 @@ __device__ __forceinline__ void norm_rotate(const AppendArgs& a, const float g[N
     for (int i = 0; i < N; ++i) ss += y[i] * y[i];
     ss = over_row<HD / N>(ss, [](T u, T w) { return u + w; });
     const T mean = ss / (T)HD + (T)a.eps;
-    const T inv = sizeof(T) == 8 ? (T)(1.0 / sqrt((double)mean)) : (T)rsqrtf((float)mean);
+    T inv;
+    if constexpr (sizeof(T) == 8) {                  // two Newton steps: 2^-50
+      inv = __builtin_amdgcn_rsq(mean);
+      inv *= 1.5 - 0.5 * mean * inv * inv;
+      inv *= 1.5 - 0.5 * mean * inv * inv;
+    } else {
+      inv = rsqrtf(mean);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] *= inv * (T)g[i];
   }
@@ -246,7 +254,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int heads, bool
     using T = std::conditional_t<KIND == KV_INT4, double, float>;
     norm_rotate<T, HD, N, NORM>(a, g, c, x);
   }
-  const int block = kv_block(a.place, t, pos);
+  const int block = kv_block(a.place, a.place.key[t], pos);
   if (block < 0) return;
   const int kh = head - a.n_h - (is_v ? a.n_kv : 0);
   store_row<HD, KIND, N>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x, l);
@@ -265,20 +273,20 @@ __global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool align
   if (unit >= 2 * a.n_kv) return;
   const bool is_v = unit >= a.n_kv;
   const int kh = is_v ? unit - a.n_kv : unit;
-  const int ti = min(t0 + (lane & 15), a.T - 1), tp = max(ti - 1, 0);
-  const int pi = a.row_pos[ti], pp = a.row_pos[tp];
-  const bool follows = ti > 0 && pp >= 0 && pi == pp + 1 && (pi & 15) != 0 && a.place.key[ti] == a.place.key[tp];
-  unsigned long long begin = __ballot(lane < 16 && t0 + lane < a.T && !follows && pi >= 0);
+  // lane i looks at row t0 - 1 + i; a row that follows the one before it in the same block is no beginning
+  const int ti = t0 - 1 + lane;
+  const bool there = ti >= 0 && ti < a.T;
+  const int pi = there ? a.row_pos[ti] : -2, ki = there ? a.place.key[ti] : -1;
+  const int pp = __shfl_up(pi, 1, 64), kp = __shfl_up(ki, 1, 64);
+  const bool follows = lane > 0 && pp >= 0 && pi == pp + 1 && (pi & 15) != 0 && ki == kp;
+  const unsigned long long chain = __ballot(follows);
+  unsigned long long begin = __ballot(lane >= 1 && lane <= 16 && pi >= 0 && !follows);
   while (begin) {
-    const int t1 = t0 + __builtin_ctzll(begin);
+    const int j = __builtin_ctzll(begin);
     begin &= begin - 1;
-    const int p1 = a.row_pos[t1], s0 = p1 & 15, key = a.place.key[t1];
-    const int block = kv_block(a.place, t1, p1);
-    if (block < 0) continue;
-    const int tn = min(t1 + (lane & 15), a.T - 1);
-    const bool in = (lane & 15) < 16 - s0 && t1 + (lane & 15) < a.T && a.place.key[tn] == key && a.row_pos[tn] == p1 + (lane & 15);
-    const int n = __builtin_ctz(~((unsigned)__ballot(in) & 0xffffu));
-    unsigned char* cell = kv_cell(a.kv, KV_INT4, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh);
+    const int t1 = t0 - 1 + j, p1 = __builtin_amdgcn_readlane(pi, j), s0 = p1 & 15;
+    const int n = 1 + __builtin_ctzll(~(chain >> (j + 1)));  // rows; the block ends them, so rows t0 - 1 .. t0 + 30 tell
+    const int block = kv_block(a.place, __builtin_amdgcn_readlane(ki, j), p1);
     float x[NI][8];
     bool live[NI], whole = true;
 #pragma unroll
@@ -288,6 +296,8 @@ __global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool align
       whole = whole && live[it];
       load_head<XBF, HD, 8>(a, aligned, live[it] ? t1 + i : t1, a.n_h + (is_v ? a.n_kv : 0) + kh, l, x[it]);
     }
+    if (block < 0) continue;
+    unsigned char* cell = kv_cell(a.kv, KV_INT4, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh);
     if (!is_v) {
 #pragma unroll
       for (int it = 0; it < NI; ++it) {
@@ -334,7 +344,7 @@ __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, in
   constexpr int LP = HD / 8;
   const int t = blockIdx.x, l = threadIdx.x % LP, kh = blockIdx.y * (256 / LP) + threadIdx.x / LP;
   if (kh >= n_kv) return;
-  const int pos = row_pos[t], block = kv_block(place, t, pos), slot = pos & 15;
+  const int pos = row_pos[t], block = kv_block(place, place.key[t], pos), slot = pos & 15;
   const size_t o = ((size_t)t * n_kv + kh) * HD;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
