@@ -65,7 +65,19 @@ enum {
    * is planned over the whole step either way, so the results are
    * bit-identical; the flag gives launch durations that are not shared with
    * concurrent kernels. */
-  MOA_FLAG_ONE_STREAM = 2
+  MOA_FLAG_ONE_STREAM = 2,
+  /* bf16 engines: K and V are cached in 4 bits (the cells of MOA_KV_INT4), 3.6
+   * (head_dim 64) to 3.8 (128) times as many positions in a byte. Every row
+   * attends to what its own position's and all earlier codes stand for, in
+   * prefill too, so chunk lengths change no value. Injected histories are
+   * stored in 4 bits from their bf16 values. EINVAL in an f32 engine. */
+  MOA_FLAG_KV_INT4 = 4,
+  /* Models with norms of queries and keys for each head before the rotation:
+   * the weight blob has q_norm[hd], k_norm[hd] after wv of each layer, and
+   * rms_eps is their eps too. */
+  MOA_FLAG_QK_NORM = 8,
+  /* Room in the arena for moa_request_scores. */
+  MOA_FLAG_SCORES = 16
 };
 
 /* Decoder geometry (Llama-style pre-norm decoder: RMSNorm, GQA attention with
@@ -130,7 +142,7 @@ moa_status moa_create(const moa_engine_cfg* cfg, void* dev_arena, size_t arena_b
  * at once, so the per-model load cost l_m of that subsection is paid once,
  * here, instead of per session). host_weights is the packed blob: tensors in the order
  *   embed[V,d], { attn_norm[d], wq[nh*hd,d], wk[nkv*hd,d], wv[nkv*hd,d],
- *   wo[d,nh*hd], mlp_norm[d], w_gate[ffn,d], w_up[ffn,d], w_down[d,ffn] } x L,
+ *   (q_norm[hd], k_norm[hd] with MOA_FLAG_QK_NORM,) wo[d,nh*hd], mlp_norm[d], w_gate[ffn,d], w_up[ffn,d], w_down[d,ffn] } x L,
  *   final_norm[d], lm_head[V,d]
  * each row-major [out, in], elements in the engine dtype (fp32, or bf16 bits),
  * no padding. The engine re-lays the matrices out for its kernels. Model ids
@@ -218,6 +230,18 @@ moa_status moa_step_noalloc(moa_engine* e, moa_step_info* info);
 moa_status moa_collect(moa_engine* e, int64_t upto_step, moa_result* res, int32_t cap,
                        int32_t* n_out, int32_t* tok_buf, int64_t tok_cap);
 
+/* Score every token that request_id emits: for output j, logprob[j] = its log
+ * probability under the logits that produced it, entropy[j] = their entropy
+ * (natural units), top_ids / top_logprobs [j][top_k] = the top_k (0 .. 32)
+ * likeliest tokens (moa_score_tokens has the definitions; top_* may be NULL
+ * when top_k is 0). The arrays are host memory of max_new_tokens (times top_k)
+ * entries that the caller keeps until the request is collected; they are
+ * complete when moa_collect returns it (or after moa_sync, for steps enqueued
+ * before). EINVAL: bad id, NULL array or top_k. ESTATE: the engine lacks
+ * MOA_FLAG_SCORES or is plan-only, or the request's prefill has completed. */
+moa_status moa_request_scores(moa_engine* e, int64_t request_id, int32_t top_k, float* logprob, float* entropy,
+                              int32_t* top_ids, float* top_logprobs);
+
 /* Wait for every enqueued step. */
 moa_status moa_sync(moa_engine* e);
 
@@ -243,6 +267,13 @@ moa_status moa_debug_request(moa_engine* e, int64_t request_id, moa_request_info
 /* The request's KV block ids (ascending, as admitted). n_out = count. */
 moa_status moa_debug_block_table(moa_engine* e, int64_t request_id, int32_t* out, int32_t cap,
                                  int32_t* n_out);
+
+/* What the cache holds of a running request: K and V of positions [0, n) of
+ * `layer`, host arrays [n][n_kv_heads][head_dim] in the engine dtype (4-bit
+ * values rounded to bf16), for a position that no step has written yet
+ * whatever its block held. Waits for the enqueued steps. EINVAL: bad id, layer
+ * or n (past the request's blocks). ESTATE: not running, or plan-only. */
+moa_status moa_debug_kv(moa_engine* e, int64_t request_id, int32_t layer, int32_t n, void* host_k, void* host_v);
 
 /* The request's prefill chunks as (step, start, length) triples. */
 moa_status moa_debug_chunks(moa_engine* e, int64_t request_id, int64_t* out, int32_t cap_triples,

@@ -339,12 +339,12 @@ __global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool align
 // ------------------------------------------------- what cached positions hold
 template <int KIND, int HD>
 __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, int layer, int n_kv, int T,
-                                                 const int* __restrict__ row_pos, KvPlace place, void* __restrict__ kout,
-                                                 void* __restrict__ vout) {
+                                                 const int* __restrict__ row_pos, int pos0, KvPlace place,
+                                                 void* __restrict__ kout, void* __restrict__ vout) {
   constexpr int LP = HD / 8;
   const int t = blockIdx.x, l = threadIdx.x % LP, kh = blockIdx.y * (256 / LP) + threadIdx.x / LP;
   if (kh >= n_kv) return;
-  const int pos = row_pos[t], block = kv_block(place, place.key[t], pos), slot = pos & 15;
+  const int pos = row_pos ? row_pos[t] : pos0 + t, block = kv_block(place, place.key ? place.key[t] : 0, pos), slot = pos & 15;
   const size_t o = ((size_t)t * n_kv + kh) * HD;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
@@ -1120,12 +1120,12 @@ hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendA
 }
 
 hipError_t launch_kv_read(hipStream_t st, int kind, const void* kv, int layer, int n_kv, int hd, int T,
-                          const int* row_pos, const KvPlace& place, void* k, void* v) {
+                          const int* row_pos, int pos0, const KvPlace& place, void* k, void* v) {
   if (T <= 0) return hipSuccess;
   if (hd != 64 && hd != 128) return hipErrorInvalidValue;
   const int heads = 2048 / hd;                       // per workgroup
   const dim3 grid(T, (n_kv + heads - 1) / heads), blk(256);
-  auto go = [&](auto kern) { klaunch(kern, grid, blk, st, kv, layer, n_kv, T, row_pos, place, k, v); };
+  auto go = [&](auto kern) { klaunch(kern, grid, blk, st, kv, layer, n_kv, T, row_pos, pos0, place, k, v); };
   if (kind == KV_F32) hd == 64 ? go(k_kv_read<KV_F32, 64>) : go(k_kv_read<KV_F32, 128>);
   else if (kind == KV_BF16) hd == 64 ? go(k_kv_read<KV_BF16, 64>) : go(k_kv_read<KV_BF16, 128>);
   else hd == 64 ? go(k_kv_read<KV_INT4, 64>) : go(k_kv_read<KV_INT4, 128>);
@@ -1182,6 +1182,20 @@ size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int 
   return n > 1 ? up256((size_t)n * T * n_h * hd * 4) + (size_t)n * T * n_h * 8 : 0;
 }
 
+static unsigned chunks4_lds(int hd) { return 4u * 64u * (unsigned)hd * 2u + 3u * 1024u; }
+static hipError_t chunks4_attributes() {
+  static bool attr = false;                // one attribute call per process for the instantiations
+  if (attr) return hipSuccess;
+  for (const void* f : {(const void*)k_attend4_chunks<64, false, false>, (const void*)k_attend4_chunks<64, false, true>,
+                        (const void*)k_attend4_chunks<64, true, true>, (const void*)k_attend4_chunks<128, false, false>,
+                        (const void*)k_attend4_chunks<128, false, true>, (const void*)k_attend4_chunks<128, true, true>}) {
+    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)chunks4_lds(128));
+    if (e != hipSuccess) return e;
+  }
+  attr = true;
+  return hipSuccess;
+}
+
 hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* workspace) {
   if (a.T <= 0) return hipSuccess;
   int nslots, split, n;
@@ -1189,17 +1203,10 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
   if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)nslots * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
   Partial4 part{nullptr, nullptr};
   if (n > 1) part = {(float*)workspace, (float*)((char*)workspace + up256((size_t)n * a.T * a.n_h * a.hd * 4))};
-  const unsigned shm = 4u * 64u * (unsigned)a.hd * 2u + 3u * 1024u;
+  const unsigned shm = chunks4_lds(a.hd);
   const bool vec = a.q_stride % (a.q_bf16 ? 8 : 4) == 0 && (uintptr_t)a.q % 16 == 0;
-  static bool attr = false;                // one attribute call per process for the instantiations
-  if (!attr) {
-    for (const void* f : {(const void*)k_attend4_chunks<64, false, false>, (const void*)k_attend4_chunks<64, false, true>,
-                          (const void*)k_attend4_chunks<128, false, false>, (const void*)k_attend4_chunks<128, false, true>}) {
-      const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * 64 * 128 * 2 + 3 * 1024);
-      if (e != hipSuccess) return e;
-    }
-    attr = true;
-  }
+  const hipError_t attr = chunks4_attributes();
+  if (attr != hipSuccess) return attr;
   const dim3 grid((unsigned)(nslots * n * a.n_kv)), blk(256);
   auto go = [&](auto kern) { klaunch_shm(kern, grid, blk, shm, st, a, (const PrefillItem*)nullptr, nslots, split, part, vec); };
   if (a.hd == 64) a.q_bf16 ? go(k_attend4_chunks<64, false, false>) : go(k_attend4_chunks<64, false, true>);
@@ -1208,5 +1215,97 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
   if (err != hipSuccess || n == 1) return err;
   if (a.hd == 64) klaunch(k_attend4_chunks_join<64>, dim3(nslots, a.n_kv), blk, st, a, n, part);
   else klaunch(k_attend4_chunks_join<128>, dim3(nslots, a.n_kv), blk, st, a, n, part);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend4_items(hipStream_t st, const Attend4Args& a, const AttnItem* items, int nitems, int split,
+                                float* pacc, float* pml) {
+  if (nitems <= 0) return hipSuccess;
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || a.q_bf16 || split > kSplit4Max || (long long)nitems * a.n_kv > INT_MAX)
+    return hipErrorInvalidValue;
+  const dim3 grid((unsigned)nitems * a.n_kv), blk(256);
+  const Partial4 part{pacc, pml};
+  if (a.hd == 64) klaunch(k_attend4_rows<64, true, true>, grid, blk, st, a, items, split, part, true);
+  else klaunch(k_attend4_rows<128, true, true>, grid, blk, st, a, items, split, part, true);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend4_prefill(hipStream_t st, const Attend4Args& a, const PrefillItem* items, int nitems) {
+  if (nitems <= 0) return hipSuccess;
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || a.q_bf16 || (long long)nitems * a.n_kv > INT_MAX)
+    return hipErrorInvalidValue;
+  const hipError_t e = chunks4_attributes();
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)nitems * a.n_kv), blk(256);
+  const Partial4 none{nullptr, nullptr};
+  const int whole = 1 << 30;                         // keys per split: all
+  if (a.hd == 64) klaunch_shm(k_attend4_chunks<64, true, true>, grid, blk, chunks4_lds(64), st, a, items, nitems, whole, none, true);
+  else klaunch_shm(k_attend4_chunks<128, true, true>, grid, blk, chunks4_lds(128), st, a, items, nitems, whole, none, true);
+  return hipGetLastError();
+}
+
+// Injected history into 4-bit cells: hd / 8 lanes a row, as for quantise(); values are rounded to
+// bf16 first, as the bf16 cache would hold them.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv4_scatter(const uint16_t* __restrict__ src, void* __restrict__ kv,
+                                                     const int* __restrict__ blocks, int p0, int layer, int kv_sel, int NB, int n_kv) {
+  constexpr int LP = HD / 8;
+  const int t = blockIdx.x, l = threadIdx.x % LP, h = blockIdx.y * (256 / LP) + threadIdx.x / LP, p = p0 + t;
+  if (h >= n_kv) return;
+  const uint16_t* s = src + ((size_t)t * n_kv + h) * HD + 4 * l;
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = bf2f(s[(i & 3) + (i >> 2) * (HD / 2)]);
+  store_row<HD, KV_INT4, 8>(kv_cell(kv, KV_INT4, HD, layer, NB, blocks[p >> 4], n_kv, h), p & 15, kv_sel != 0, x, l);
+}
+
+// The values of k_kv_fill: a workgroup per (KV block, layer).
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv4_fill(void* __restrict__ kv, const int* __restrict__ bt_store,
+                                                  const FillReq* __restrict__ reqs, int nreqs, int NB, int n_kv) {
+  constexpr int LP = HD / 8;
+  const int item = blockIdx.x, layer = blockIdx.y, l = threadIdx.x % LP;
+  int lo = 0, hi = nreqs - 1;                        // the last entry with item0 <= item
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (reqs[mid].item0 <= item) lo = mid;
+    else hi = mid - 1;
+  }
+  const FillReq rq = reqs[lo];
+  const int b = item - rq.item0, block = bt_store[rq.bt_off + b];
+  const uint32_t tg = rq.tag * 0x9e3779b9u;
+  for (int row = threadIdx.x / LP; row < n_kv * 2 * kBlock; row += 256 / LP) {
+    const int head = row / (2 * kBlock), kv_sel = (row / kBlock) & 1, slot = row & (kBlock - 1), p = b * kBlock + slot;
+    if (p >= rq.ctx) continue;
+    const uint32_t hp = tg ^ mix32(((uint32_t)(layer * 2 + kv_sel) << 24) ^ (uint32_t)p);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int rem = head * HD + 4 * l + (i & 3) + (i >> 2) * (HD / 2);
+      const uint32_t u = mix32(hp ^ (uint32_t)(rem * 0x85ebca6bu));
+      x[i] = bf2f(f2bf((float)(int)(u >> 8) * (1.0f / 8388608.0f) - 1.0f));
+    }
+    store_row<HD, KV_INT4, 8>(kv_cell(kv, KV_INT4, HD, layer, NB, block, n_kv, head), slot, kv_sel != 0, x, l);
+  }
+}
+
+hipError_t launch_kv4_scatter(hipStream_t st, const void* src, void* kv, const int* blocks, int p0, int n, int layer,
+                              int kv_sel, int num_blocks, int n_kv, int hd) {
+  if (n <= 0) return hipSuccess;
+  if (hd != 64 && hd != 128) return hipErrorInvalidValue;
+  const int heads = 2048 / hd;                       // per workgroup
+  const dim3 grid(n, (n_kv + heads - 1) / heads), blk(256);
+  if (hd == 64) klaunch(k_kv4_scatter<64>, grid, blk, st, (const uint16_t*)src, kv, blocks, p0, layer, kv_sel, num_blocks, n_kv);
+  else klaunch(k_kv4_scatter<128>, grid, blk, st, (const uint16_t*)src, kv, blocks, p0, layer, kv_sel, num_blocks, n_kv);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_fill(hipStream_t st, void* kv, const int* bt_store, const FillReq* reqs, int nreqs, int nitems,
+                           int n_layers, int num_blocks, int n_kv, int hd) {
+  if (nitems <= 0) return hipSuccess;
+  if (nreqs < 1 || (hd != 64 && hd != 128) || n_layers > 65535) return hipErrorInvalidValue;
+  const dim3 grid(nitems, n_layers), blk(256);
+  if (hd == 64) klaunch(k_kv4_fill<64>, grid, blk, st, kv, bt_store, reqs, nreqs, num_blocks, n_kv);
+  else klaunch(k_kv4_fill<128>, grid, blk, st, kv, bt_store, reqs, nreqs, num_blocks, n_kv);
   return hipGetLastError();
 }

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <array>
+#include <climits>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -78,12 +79,17 @@ struct Request {
   std::vector<std::array<int64_t, 3>> chunks;
   int state = 0;                      // 0 pending, 1 running, 2 retired, 3 collected
   float* capture = nullptr;
+  // token scores (moa_request_scores): host arrays of G and G * top entries
+  bool scored = false;
+  int32_t top = 0;
+  float *logprob = nullptr, *entropy = nullptr, *top_lps = nullptr;
+  int32_t* top_ids = nullptr;
 };
 
 struct ModelDev {
   // device pointers (bf16 bits or f32)
   const void* embed = nullptr;
-  std::vector<const void*> attn_norm, wqkv, wo, mlp_norm, wgu, wdown;
+  std::vector<const void*> attn_norm, wqkv, q_norm, k_norm, wo, mlp_norm, wgu, wdown;   // q_norm, k_norm: MOA_FLAG_QK_NORM
   const void* final_norm = nullptr;
   const void* lm_head = nullptr;
 };
@@ -131,7 +137,7 @@ struct Layout {
   size_t model_bytes, kv_bytes, block_bytes;
   size_t off_xpart[kMaxShares - 1];   // split-K partials of shares 1.. (0: none)
   size_t off_kv, off_tok, off_bt, off_rope, off_meta, off_x, off_xn, off_part, off_q, off_ao, off_h,
-      off_logits, off_xl, off_pacc, off_pml, off_models, total;
+      off_logits, off_xl, off_pacc, off_pml, off_scores, off_score_ws, off_models, total;
   int64_t token_store, block_store, meta_ints;
 };
 
@@ -157,7 +163,19 @@ bool valid_cfg(const moa_engine_cfg& c) {
   if (c.num_kv_blocks < 1 || c.max_num_seqs < 1 || c.max_prefill_tokens < 0 || c.max_model_len < 2) return false;
   if (c.max_models < 1 || c.max_models > kMaxModels) return false;
   if (c.token_store < 0 || c.block_store < 0) return false;
+  if ((c.flags & MOA_FLAG_KV_INT4) && c.dtype != MOA_BF16) return false;
   return true;
+}
+
+// Keys per decode-attention split, and rows per prefill block, of the engine's cache
+// (4-bit: a workgroup brings a KV head's 128 queries; splits as fixed as the others).
+constexpr int kSplitKeys4 = 1024;
+int split_keys(const moa_engine_cfg& c) { return c.flags & MOA_FLAG_KV_INT4 ? kSplitKeys4 : kSplitKeys; }
+int prefill_rows(const moa_engine_cfg& c) {
+  return c.flags & MOA_FLAG_KV_INT4 ? kPrefillRows / (c.model.n_heads / c.model.n_kv_heads) : kPrefillRows;
+}
+int kv_kind(const moa_engine_cfg& c) {
+  return c.dtype != MOA_BF16 ? KV_F32 : (c.flags & MOA_FLAG_KV_INT4 ? KV_INT4 : KV_BF16);
 }
 
 Layout make_layout(const moa_engine_cfg& c) {
@@ -169,7 +187,7 @@ Layout make_layout(const moa_engine_cfg& c) {
   const int64_t qkv = (nh + 2 * nkv) * hd;
   L.Tmax = (int64_t)c.max_prefill_tokens + c.max_num_seqs;
   L.Rmax = c.max_num_seqs;
-  L.slots_cap = (int64_t)c.num_kv_blocks * kBlock / kSplitKeys + c.max_num_seqs + 1;
+  L.slots_cap = (int64_t)c.num_kv_blocks * kBlock / split_keys(c) + c.max_num_seqs + 1;
   L.items_cap = L.Tmax + L.slots_cap;
   L.red_cap = c.max_num_seqs;
   // split-K partials: a prefill-sized step unsplit, or a full decode batch
@@ -178,10 +196,11 @@ Layout make_layout(const moa_engine_cfg& c) {
   L.token_store = c.token_store ? c.token_store : (int64_t)64 << 20;
   L.block_store = c.block_store ? c.block_store : (int64_t)16 << 20;
   L.meta_ints = 4 * L.Tmax + 2 * L.Rmax + 8 * L.items_cap + 4 * L.red_cap + 4 * L.Tmax + 4 * L.Rmax;
-  L.block_bytes = (size_t)Lr * nkv * 2 * kBlock * hd * L.esz;
+  L.block_bytes = (size_t)Lr * nkv * kv_cell_bytes(kv_kind(c), (int)hd);
   L.kv_bytes = L.block_bytes * (size_t)c.num_kv_blocks;
   const size_t per_layer = (size_t)(2 * d + qkv * d + d * nh * hd + 3 * F * d) * L.esz;
-  L.model_bytes = align_up((size_t)(2 * V * d + d) * L.esz + 256 * (8 + 6 * Lr) + per_layer * Lr, kModelAlign);
+  const size_t qk = c.flags & MOA_FLAG_QK_NORM ? 2 * align_up((size_t)hd * L.esz, 256) : 0;   // per layer
+  L.model_bytes = align_up((size_t)(2 * V * d + d) * L.esz + 256 * (8 + 6 * Lr) + (per_layer + qk) * Lr, kModelAlign);
 
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
@@ -207,6 +226,9 @@ Layout make_layout(const moa_engine_cfg& c) {
   L.off_xl = take((size_t)2 * L.Rmax * d * L.esz);
   L.off_pacc = take((size_t)L.slots_cap * nh * hd * 4);
   L.off_pml = take((size_t)L.slots_cap * nh * 2 * 4);
+  const bool scores = (c.flags & MOA_FLAG_SCORES) != 0;
+  L.off_scores = scores ? take((size_t)L.Rmax * (2 + 2 * MOA_MAX_TOP) * 4) : 0;
+  L.off_score_ws = scores ? take(score_bytes_max((int)V)) : 0;
   L.off_models = align_up(off, kModelAlign);
   L.total = L.off_models + L.model_bytes * (size_t)c.max_models;
   return L;
@@ -259,6 +281,13 @@ struct moa_engine {
   float* pacc = nullptr;
   float* pml = nullptr;
   void* scratch = nullptr;            // this GPU's library scratch array (moa_step_noalloc)
+  float* scores = nullptr;            // a step's token scores: [R] log probability, [R] entropy, [R][k] ids, [R][k] log probabilities
+  void* score_ws = nullptr;
+  // scores of the step in a staging slot, until they are handed to the requests' arrays
+  struct Score { int64_t id; int row, gen; };
+  float* score_host[kStageSlots] = {};
+  std::vector<Score> score_rows[kStageSlots];
+  int score_R[kStageSlots] = {}, score_k[kStageSlots] = {};
 
   // pinned staging ring and per-step completion events
   struct Stage { char* buf = nullptr; size_t cap = 0; };
@@ -732,6 +761,10 @@ moa_status moa_create(const moa_engine_cfg* cfg, void* dev_arena, size_t arena_b
     e->xl = A + L.off_xl;
     e->pacc = (float*)(A + L.off_pacc);
     e->pml = (float*)(A + L.off_pml);
+    if (L.off_scores) {
+      e->scores = (float*)(A + L.off_scores);
+      e->score_ws = A + L.off_score_ws;
+    }
     hipError_t err = hipStreamCreateWithFlags(&e->copy_stream, hipStreamNonBlocking);
     for (int i = 0; i < kStageSlots && err == hipSuccess; ++i) err = hipEventCreateWithFlags(&e->ev[i], hipEventDisableTiming);
     if (err == hipSuccess && e->xpart[0]) err = hipEventCreateWithFlags(&e->ev_fork, hipEventDisableTiming);
@@ -759,6 +792,8 @@ moa_status moa_create(const moa_engine_cfg* cfg, void* dev_arena, size_t arena_b
       const size_t cap = std::max((size_t)L.meta_ints * 4, (size_t)1 << 20);
       err = hipHostMalloc((void**)&e->stage[i].buf, cap, hipHostMallocDefault);
       if (err == hipSuccess) e->stage[i].cap = cap;
+      if (err == hipSuccess && L.off_scores)
+        err = hipHostMalloc((void**)&e->score_host[i], (size_t)L.Rmax * (2 + 2 * MOA_MAX_TOP) * 4, hipHostMallocDefault);
     }
     if (err != hipSuccess) {
       hip_fail(nullptr, err, "moa_create");
@@ -778,6 +813,7 @@ void moa_destroy(moa_engine* e) {
       if (x) (void)hipStreamSynchronize(x);
     for (int i = 0; i < kStageSlots; ++i) {
       if (e->stage[i].buf) (void)hipHostFree(e->stage[i].buf);
+      if (e->score_host[i]) (void)hipHostFree(e->score_host[i]);
       if (e->ev[i]) (void)hipEventDestroy(e->ev[i]);
     }
     if (e->pinned_out) (void)hipHostFree(e->pinned_out);
@@ -807,7 +843,8 @@ moa_status moa_load_expert(moa_engine* e, const moa_model_cfg* mc, const void* h
   const int64_t d = g.d_model, hd = g.head_dim, nh = g.n_heads, nkv = g.n_kv_heads, V = g.vocab, F = g.ffn_dim,
                 Lr = g.n_layers;
   const int64_t qd = nh * hd, kd = nkv * hd, qkv = qd + 2 * kd;
-  const size_t expect = (size_t)(2 * V * d + d + Lr * (2 * d + qkv * d + d * qd + 3 * F * d)) * esz;
+  const bool qk_norm = (e->cfg.flags & MOA_FLAG_QK_NORM) != 0;
+  const size_t expect = (size_t)(2 * V * d + d + Lr * (2 * d + qkv * d + d * qd + 3 * F * d + (qk_norm ? 2 * hd : 0))) * esz;
   if (nbytes != expect) return MOA_EINVAL;
   if ((int)e->models.size() >= e->cfg.max_models) return MOA_ENOMEM;
 
@@ -853,6 +890,8 @@ moa_status moa_load_expert(moa_engine* e, const moa_model_cfg* mc, const void* h
     const char* wq = next(qd * d);
     const char* wk = next(kd * d);
     const char* wv = next(kd * d);
+    const char* qn = qk_norm ? next(hd) : nullptr;
+    const char* kn = qk_norm ? next(hd) : nullptr;
     const char* wo = next(d * qd);
     const char* mn = next(d);
     const char* wg = next(F * d);
@@ -864,6 +903,10 @@ moa_status moa_load_expert(moa_engine* e, const moa_model_cfg* mc, const void* h
       if (n < qd + kd) return wk + (size_t)(n - qd) * d * esz;
       return wv + (size_t)(n - qd - kd) * d * esz;
     })));
+    if (qk_norm) {
+      M.q_norm.push_back(chk(put_raw(qn, hd)));
+      M.k_norm.push_back(chk(put_raw(kn, hd)));
+    }
     M.wo.push_back(chk(put_mat(d, qd, [&](int64_t n) { return wo + (size_t)n * qd * esz; })));
     M.mlp_norm.push_back(chk(put_raw(mn, d)));
     if (e->bf16) {
@@ -975,9 +1018,12 @@ moa_status write_histories(moa_engine* e, const std::vector<int64_t>& admitted, 
   const size_t row = (size_t)g.n_kv_heads * g.head_dim;             // elements per position
   const size_t cap_rows = std::max<size_t>(1, (size_t)e->lay.Rmax * g.vocab * 4 / (row * esz));
   bool drained = false;
+  const bool kv4 = kv_kind(e->cfg) == KV_INT4;
   if (nfills > 0)
-    HIPCHK(launch_kv_fill(e->stream, e->bf16, e->kv, e->bt_store, dev_fills, nfills, nitems, g.n_layers,
-                          e->cfg.num_kv_blocks, g.n_kv_heads, g.head_dim), "history fill");
+    HIPCHK(kv4 ? launch_kv4_fill(e->stream, e->kv, e->bt_store, dev_fills, nfills, nitems, g.n_layers,
+                                 e->cfg.num_kv_blocks, g.n_kv_heads, g.head_dim)
+               : launch_kv_fill(e->stream, e->bf16, e->kv, e->bt_store, dev_fills, nfills, nitems, g.n_layers,
+                                e->cfg.num_kv_blocks, g.n_kv_heads, g.head_dim), "history fill");
   for (int64_t id : admitted) {
     Request& r = e->reqs[id];
     if (!r.history || r.shift == 0 || r.host_kv.empty()) continue;
@@ -991,8 +1037,10 @@ moa_status write_histories(moa_engine* e, const std::vector<int64_t>& admitted, 
           const size_t n = std::min(cap_rows, (size_t)r.shift - p0);
           const char* src = r.host_kv.data() + (((size_t)l * 2 + kv) * r.shift + p0) * row * esz;
           HIPCHK(hipMemcpy(e->logits, src, n * row * esz, hipMemcpyHostToDevice), "history upload");
-          HIPCHK(launch_kv_scatter(e->stream, e->bf16, e->logits, e->kv, e->bt_store + r.bt_off, (int)p0, (int)n, l,
-                                   kv, e->cfg.num_kv_blocks, g.n_kv_heads, g.head_dim), "history scatter");
+          HIPCHK(kv4 ? launch_kv4_scatter(e->stream, e->logits, e->kv, e->bt_store + r.bt_off, (int)p0, (int)n, l, kv,
+                                          e->cfg.num_kv_blocks, g.n_kv_heads, g.head_dim)
+                     : launch_kv_scatter(e->stream, e->bf16, e->logits, e->kv, e->bt_store + r.bt_off, (int)p0, (int)n,
+                                         l, kv, e->cfg.num_kv_blocks, g.n_kv_heads, g.head_dim), "history scatter");
           HIPCHK(hipStreamSynchronize(e->stream), "history sync");
         }
     std::vector<char>().swap(r.host_kv);
@@ -1000,9 +1048,25 @@ moa_status write_histories(moa_engine* e, const std::vector<int64_t>& admitted, 
   return MOA_OK;
 }
 
+// Hand the scores of a completed step in staging slot `slot` to its requests' arrays.
+void deliver_scores(moa_engine* e, int slot) {
+  const float* p = e->score_host[slot];
+  const int R = e->score_R[slot], k = e->score_k[slot];
+  for (const moa_engine::Score& s : e->score_rows[slot]) {
+    const Request& r = e->reqs[s.id];
+    r.logprob[s.gen] = p[s.row];
+    r.entropy[s.gen] = p[R + s.row];
+    if (r.top == 0) continue;
+    std::memcpy(r.top_ids + (size_t)s.gen * r.top, p + 2 * (size_t)R + (size_t)s.row * k, (size_t)r.top * 4);
+    std::memcpy(r.top_lps + (size_t)s.gen * r.top, p + (2 + (size_t)k) * R + (size_t)s.row * k, (size_t)r.top * 4);
+  }
+  e->score_rows[slot].clear();
+}
+
 // Wait until staging slot `slot` is no longer read by an in-flight step.
 moa_status wait_slot(moa_engine* e, int slot) {
   if (e->ev_step[slot] >= 0) HIPCHK(hipEventSynchronize(e->ev[slot]), "staging wait");
+  deliver_scores(e, slot);
   return MOA_OK;
 }
 
@@ -1037,13 +1101,15 @@ size_t noalloc_scratch_bytes(const moa_engine* e) {
 }
 
 moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int T, int R,
-                        const int* grp_rows, const int* grp_lm, bool noalloc) {
+                        const int* grp_rows, const int* grp_lm, bool noalloc,
+                        std::vector<moa_engine::Score>& score_rows) {
   const moa_model_cfg& g = e->cfg.model;
   const Layout& L = e->lay;
   const int slot = (int)(e->step_idx % kStageSlots);
   moa_status st = wait_slot(e, slot);
   if (st != MOA_OK) return st;
   e->keepalive[slot].clear();                 // the step that read them has completed
+  e->score_rows[slot].swap(score_rows);
 
   // partial sums: the arena's workspace, or this GPU's library scratch
   float* part = e->part;
@@ -1178,6 +1244,9 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     if (rs != MOA_OK) return rs;
   }
   const double esz = (double)L.esz;
+  const int kind = kv_kind(e->cfg);
+  const double key_bytes = (double)kv_cell_bytes(kind, hd) / kBlock;     // K and V of a position and KV head
+  const bool kv4 = kind == KV_INT4, qk_norm = (e->cfg.flags & MOA_FLAG_QK_NORM) != 0;
   // algorithmic bytes / flops of one grouped GEMM launch
   auto gemm_cost = [&](const GemmArgs& a, int epi, double& bytes, double& flops) {
     double rows = 0;
@@ -1199,7 +1268,7 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     const ReduceItem* red;
     const PrefillItem* pre;
     int nitems, nred, npre, max_item_blocks, pre_max_keys;
-    double attn_bytes, attn_flops, pre_bytes, pre_flops, red_bytes;
+    double attn_bytes, attn_flops, pre_bytes, pre_flops, red_bytes, pre_rows;
     int prev_split;
     size_t prev_stride;
   };
@@ -1239,9 +1308,10 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     }
     double nsl = 0;
     for (int i = d0; i < d0 + b.nred; ++i) nsl += e->red[i].nslots;
-    b.pre_bytes = pre_keys * nkv * 2.0 * hd * esz + pre_rows * nh * hd * 8.0;
+    b.pre_bytes = pre_keys * nkv * key_bytes + pre_rows * nh * hd * 8.0;
     b.pre_flops = pre_pairs * nh * hd * 4.0;
-    b.attn_bytes = kv_keys * nkv * 2.0 * hd * esz + (double)b.nr * nh * hd * 8.0;
+    b.pre_rows = pre_rows;
+    b.attn_bytes = kv_keys * nkv * key_bytes + (double)b.nr * nh * hd * 8.0;
     b.attn_flops = kv_keys * nh * hd * 4.0;
     b.red_bytes = nsl * nh * (hd + 2) * 4.0;
     b.prev_split = 0;
@@ -1263,6 +1333,9 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     // decides alike): the row GEMMs take over the norms, residuals and RoPE between
     // the layers' GEMMs; the final norm reads the finished residual.
     const bool row_gemms = bf && T <= kRowSteps && (int64_t)T * F <= (int64_t)kRowDepth * d;
+    // (their qkv GEMM knows neither per-head norms nor 4-bit cells: those keep the norm and
+    // append launches around the small-row GEMM)
+    const bool row_qkv = row_gemms && !kv4 && !qk_norm;
     for (int l = 0; l < g.n_layers; ++l) {
       for (int u = 0; u < nshare; ++u) {
         Share& b = sh[u];
@@ -1301,13 +1374,13 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
         auto row_norm = [&](auto get) {
           for (int k = 0; k < b.ng; ++k) ra.gamma.p[k] = get(e->models[gmodel[b.g0 + k]]);
         };
-        if (!row_gemms)
+        if (!row_qkv)
           LAUNCH(MOA_K_NORM, norm_bytes + b.prev_split * (double)b.nr * d * 4.0, 0,
                launch_add_rmsnorm(st, bf, e->x + ro * d, b.prev_split ? b.part + ro * d : nullptr, b.prev_split,
                                   b.prev_stride, nullptr, sd.row_model + ro, b.nr,
                                   fill([l](const ModelDev& x) { return x.attn_norm[l]; }), xn_b, xn_lo, d,
                                   g.rms_eps), "attn norm");
-        if (row_gemms) {
+        if (row_qkv) {
           row_norm([l](const ModelDev& x) { return x.attn_norm[l]; });
           RowArgs rq = ra;
           rq.row_pos = sd.row_pos;
@@ -1329,17 +1402,71 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
                     xn_lo, b.part, nullptr, 0, true, ga, mt, nt, lg);
           gemm_cost(ga, EPI_F32, gb, gf);
           LAUNCH_GEMM(MOA_K_GEMM_QKV, lg, gb, gf, launch_gemm(st, bf, ga, EPI_F32, mt, nt), "qkv gemm");
-          LAUNCH(MOA_K_ROPE_KV, (double)b.nr * qkv * 4.0 * ga.S + (double)b.nr * (nh * hd * 4.0 + 2.0 * nkv * hd * esz), 0,
-                 launch_rope_kv(st, bf, b.part + ro * qkv, ga.S, ga.out_split, sd.row_pos + ro, sd.row_bt + ro,
-                                e->bt_store, e->rope, e->q + ro * nh * hd, e->kv, l, e->cfg.num_kv_blocks, nh, nkv, hd,
-                                b.nr), "rope kv");
+          const double rope_bytes = (double)b.nr * qkv * 4.0 * ga.S + (double)b.nr * (nh * hd * 4.0 + nkv * key_bytes);
+          if (kv4 || qk_norm) {
+            AppendArgs ap{};
+            ap.x = b.part + ro * qkv;
+            ap.stride = qkv;
+            ap.nsplit = ga.S;
+            ap.split_stride = ga.out_split;
+            ap.row_pos = sd.row_pos + ro;
+            ap.place = KvPlace{e->bt_store, sd.row_bt + ro, 1, INT_MAX, INT_MAX, e->cfg.num_kv_blocks};
+            ap.rope = e->rope;
+            ap.rope_len = e->cfg.max_model_len;
+            if (qk_norm) {
+              for (int m = 0; m < M; ++m) {
+                ap.q_gain.p[m] = e->models[m].q_norm[l];
+                ap.k_gain.p[m] = e->models[m].k_norm[l];
+              }
+              ap.row_model = sd.row_model + ro;
+              ap.gain_bf16 = bf;
+              ap.eps = g.rms_eps;
+            }
+            ap.q = e->q + ro * nh * hd;
+            ap.kv = e->kv;
+            ap.layer = l;
+            ap.n_h = nh;
+            ap.n_kv = nkv;
+            ap.hd = hd;
+            ap.T = b.nr;
+            ap.runs = 2.0 * b.pre_rows > b.nr;
+            LAUNCH(MOA_K_ROPE_KV, rope_bytes, 0, launch_kv_append(st, false, kind, ap), "kv append");
+          } else {
+            LAUNCH(MOA_K_ROPE_KV, rope_bytes, 0,
+                   launch_rope_kv(st, bf, b.part + ro * qkv, ga.S, ga.out_split, sd.row_pos + ro, sd.row_bt + ro,
+                                  e->bt_store, e->rope, e->q + ro * nh * hd, e->kv, l, e->cfg.num_kv_blocks, nh, nkv, hd,
+                                  b.nr), "rope kv");
+          }
         }
-        if (b.npre > 0)
+        Attend4Args a4{};
+        if (kv4) {
+          a4.q = e->q;
+          a4.q_stride = (size_t)nh * hd;
+          a4.out = e->ao;
+          a4.out_lo = ao_lo;
+          a4.out_type = OUT_SPLIT;
+          a4.kv = e->kv;
+          a4.layer = l;
+          a4.num_blocks = e->cfg.num_kv_blocks;
+          a4.n_h = nh;
+          a4.n_kv = nkv;
+          a4.hd = hd;
+          a4.scale = 1.0f / std::sqrt((float)hd);
+          a4.tables = e->bt_store;
+          a4.T = T;
+        }
+        if (b.npre > 0 && kv4)
+          LAUNCH(MOA_K_PREFILL_ATTN, b.pre_bytes, b.pre_flops, launch_attend4_prefill(st, a4, b.pre, b.npre),
+                 "4-bit prefill attention");
+        else if (b.npre > 0)
           LAUNCH(MOA_K_PREFILL_ATTN, b.pre_bytes, b.pre_flops,
                  launch_prefill_attention(st, b.pre, b.npre, b.pre_max_keys, e->q, e->kv, e->bt_store, l,
                                           e->cfg.num_kv_blocks, nh, nkv, hd, 1.0f / std::sqrt((float)hd), e->ao,
                                           ao_lo), "prefill attention");
-        if (b.nitems > 0)
+        if (b.nitems > 0 && kv4)
+          LAUNCH(MOA_K_ATTN, b.attn_bytes, b.attn_flops,
+                 launch_attend4_items(st, a4, b.items, b.nitems, kSplitKeys4, pacc, pml), "4-bit attention");
+        else if (b.nitems > 0)
           LAUNCH(MOA_K_ATTN, b.attn_bytes, b.attn_flops,
                  launch_attention(st, bf, b.items, b.nitems, b.max_item_blocks, e->q, e->kv, e->bt_store, sd.row_bt,
                                   l, e->cfg.num_kv_blocks, nh, nkv, hd, 1.0f / std::sqrt((float)hd), e->ao, ao_lo,
@@ -1430,6 +1557,42 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     for (int u = 1; u < nshare; ++u) {
       HIPCHK(hipEventRecord(e->ev_join[u - 1], e->xs[u - 1]), "stream join");
       HIPCHK(hipStreamWaitEvent(s, e->ev_join[u - 1], 0), "stream join");
+    }
+    // Token scores of the rows that ask for them, in runs of neighbouring rows (one
+    // run over the rows between where there would be many), and one copy to the host.
+    std::vector<moa_engine::Score>& want = e->score_rows[slot];
+    if (!want.empty()) {
+      int k = 0;
+      for (const moa_engine::Score& w : want) k = std::max(k, e->reqs[w.id].top);
+      e->score_R[slot] = R;
+      e->score_k[slot] = k;
+      ScoreArgs sa{};
+      sa.logits = e->logits;
+      sa.stride = V;
+      sa.vocab = V;
+      sa.top = k;
+      std::vector<std::array<int, 2>> runs;
+      for (const moa_engine::Score& w : want) {
+        if (!runs.empty() && runs.back()[1] == w.row) runs.back()[1]++;
+        else runs.push_back({w.row, w.row + 1});
+      }
+      if (runs.size() > 8) runs.assign(1, {want.front().row, want.back().row + 1});
+      float* lp = e->scores;
+      for (const auto& run : runs) {
+        ScoreArgs x = sa;
+        const size_t r = (size_t)run[0];
+        x.rows = run[1] - run[0];
+        x.logits = e->logits + r * V;
+        x.tokens = e->tok_store;
+        x.token_at = sd.lm_dst + r;
+        x.logprob = lp + r;
+        x.entropy = lp + R + r;
+        x.top_ids = (int*)(lp + 2 * (size_t)R + r * k);
+        x.top_logprobs = lp + (2 + (size_t)k) * R + r * k;
+        LAUNCH(MOA_K_ARGMAX, (double)x.rows * V * 4.0, 0, launch_score(s, x, e->score_ws), "token scores");
+      }
+      HIPCHK(hipMemcpyAsync(e->score_host[slot], e->scores, (size_t)R * (2 + 2 * k) * 4, hipMemcpyDeviceToHost, s),
+             "score download");
     }
   }
   (void)L;
@@ -1560,6 +1723,8 @@ moa_status step_impl(moa_engine* e, moa_step_info* info, bool noalloc) {
   int grp_rows[kMaxModels] = {0}, grp_lm[kMaxModels] = {0};
   int nslots = 0;
   std::vector<std::pair<int64_t, int>> capture_rows;   // (request, lm row)
+  std::vector<moa_engine::Score> score_rows;
+  const int SK = split_keys(e->cfg), PR = prefill_rows(e->cfg);
   for (int mi = 0; mi < M; ++mi) {
     const int m = e->morder[mi];
     for (int pass = 0; pass < 2; ++pass) {
@@ -1578,18 +1743,17 @@ moa_status step_impl(moa_engine* e, moa_step_info* info, bool noalloc) {
           const int ctx = pos + 1;
           const int bto = (int)r.bt_off;
           if (a.kind == 0 && tiled_prefill) {
-            if (i % kPrefillRows == 0) e->pitems.push_back({row, pos, std::min(kPrefillRows, a.len - i), bto});
+            if (i % PR == 0) e->pitems.push_back({row, pos, std::min(PR, a.len - i), bto});
           } else if (a.kind == 0) {
             e->items.push_back({row, 0, ctx, -1, bto, 0, 0, 0});
           } else {
-            const int ns = (ctx + kSplitKeys - 1) / kSplitKeys;
+            const int ns = (ctx + SK - 1) / SK;
             if (ns == 1) {
               e->items.push_back({row, 0, ctx, -1, bto, 0, 0, 0});
             } else {
               e->red.push_back({row, nslots, ns, 0});
               for (int k = 0; k < ns; ++k)
-                e->items.push_back({row, k * kSplitKeys, std::min(ctx, (k + 1) * kSplitKeys), nslots + k,
-                                    bto + k * kSplitKeys / kBlock, 0, 0, 0});
+                e->items.push_back({row, k * SK, std::min(ctx, (k + 1) * SK), nslots + k, bto + k * SK / kBlock, 0, 0, 0});
               nslots += ns;
             }
           }
@@ -1600,6 +1764,7 @@ moa_status step_impl(moa_engine* e, moa_step_info* info, bool noalloc) {
             e->l_dst.push_back((int)(r.tok_off + r.P - r.shift + gen_idx));
             grp_lm[m]++;
             if (r.capture) capture_rows.push_back({a.id, (int)e->l_src.size() - 1});
+            if (r.scored) score_rows.push_back({a.id, (int)e->l_src.size() - 1, gen_idx});
           }
         }
       }
@@ -1663,7 +1828,7 @@ moa_status step_impl(moa_engine* e, moa_step_info* info, bool noalloc) {
       std::fprintf(stderr, "moa: step plan exceeds workspace (T=%d R=%d slots=%d)\n", T, R, nslots);
       return MOA_EHIP;
     }
-    moa_status st = enqueue_step(e, admitted, T, R, grp_rows, grp_lm, noalloc);
+    moa_status st = enqueue_step(e, admitted, T, R, grp_rows, grp_lm, noalloc, score_rows);
     if (st != MOA_OK) return st;
     for (auto& cr : capture_rows) {
       Request& r = e->reqs[cr.first];
@@ -1754,6 +1919,8 @@ moa_status moa_collect(moa_engine* e, int64_t upto_step, moa_result* res, int32_
     // been reused since, that step already completed), then copy on the side stream.
     for (int i = 0; i < kStageSlots; ++i)
       if (e->ev_step[i] == last) HIPCHK(hipEventSynchronize(e->ev[i]), "collect wait");
+    for (int i = 0; i < kStageSlots; ++i)
+      if (e->ev_step[i] <= last) deliver_scores(e, i);
     // tokens, then the table of runs one launch copies them by
     const size_t need = align_up((size_t)ntok, 4) + 4 * (size_t)n;
     if (need > e->pinned_out_cap) {
@@ -1788,6 +1955,7 @@ moa_status moa_collect(moa_engine* e, int64_t upto_step, moa_result* res, int32_
     o += r.G;
     r.state = 3;
     r.capture = nullptr;
+    r.scored = false;
     e->live -= 1;
   }
   e->done.erase(e->done.begin(), e->done.begin() + n);
@@ -1797,7 +1965,27 @@ moa_status moa_collect(moa_engine* e, int64_t upto_step, moa_result* res, int32_
 moa_status moa_sync(moa_engine* e) {
   if (!e) return MOA_EINVAL;
   if (e->broken) return MOA_ESTATE;
-  if (!e->plan_only) HIPCHK(hipStreamSynchronize(e->stream), "sync");
+  if (!e->plan_only) {
+    HIPCHK(hipStreamSynchronize(e->stream), "sync");
+    for (int i = 0; i < kStageSlots; ++i) deliver_scores(e, i);
+  }
+  return MOA_OK;
+}
+
+moa_status moa_request_scores(moa_engine* e, int64_t id, int32_t top_k, float* logprob, float* entropy,
+                              int32_t* top_ids, float* top_logprobs) {
+  if (!e || id < 0 || id >= (int64_t)e->reqs.size() || !logprob || !entropy) return MOA_EINVAL;
+  if (top_k < 0 || top_k > MOA_MAX_TOP || top_k > e->cfg.model.vocab || (top_k > 0 && (!top_ids || !top_logprobs)))
+    return MOA_EINVAL;
+  if (e->broken || e->plan_only || !(e->cfg.flags & MOA_FLAG_SCORES)) return MOA_ESTATE;
+  Request& r = e->reqs[id];
+  if (r.state >= 2 || (r.pre == r.P && r.gen > 0)) return MOA_ESTATE;
+  r.scored = true;
+  r.top = top_k;
+  r.logprob = logprob;
+  r.entropy = entropy;
+  r.top_ids = top_ids;
+  r.top_lps = top_logprobs;
   return MOA_OK;
 }
 
@@ -1821,6 +2009,30 @@ moa_status moa_debug_block_table(moa_engine* e, int64_t id, int32_t* out, int32_
   *n_out = (int32_t)r.blocks.size();
   if ((int32_t)r.blocks.size() > cap || (!out && !r.blocks.empty())) return MOA_EINVAL;
   if (!r.blocks.empty()) std::memcpy(out, r.blocks.data(), r.blocks.size() * 4);
+  return MOA_OK;
+}
+
+moa_status moa_debug_kv(moa_engine* e, int64_t id, int32_t layer, int32_t n, void* host_k, void* host_v) {
+  if (!e || id < 0 || id >= (int64_t)e->reqs.size() || layer < 0 || layer >= e->cfg.model.n_layers || n < 0) return MOA_EINVAL;
+  const Request& r = e->reqs[id];
+  if (n > (int64_t)r.need * kBlock || (n > 0 && (!host_k || !host_v))) return MOA_EINVAL;
+  if (e->broken || e->plan_only || r.state != 1) return MOA_ESTATE;
+  const moa_model_cfg& g = e->cfg.model;
+  const size_t row = (size_t)g.n_kv_heads * g.head_dim * e->lay.esz;        // bytes of a position's K
+  const size_t cap = (size_t)e->lay.Rmax * g.vocab * 4 / (2 * row);         // positions the logits workspace holds
+  if (cap == 0) return MOA_ENOMEM;
+  HIPCHK(hipStreamSynchronize(e->stream), "kv read");
+  for (size_t p = 0; p < (size_t)n; p += cap) {
+    const size_t m = std::min(cap, (size_t)n - p);
+    char* k = (char*)e->logits;
+    char* v = k + align_up(m * row, 16);
+    const KvPlace at{e->bt_store + r.bt_off, nullptr, 0, 1, r.need, e->cfg.num_kv_blocks};
+    HIPCHK(launch_kv_read(e->stream, kv_kind(e->cfg), e->kv, layer, g.n_kv_heads, g.head_dim, (int)m, nullptr, (int)p, at, k, v),
+           "kv read");
+    HIPCHK(hipStreamSynchronize(e->stream), "kv read");
+    HIPCHK(hipMemcpy((char*)host_k + p * row, k, m * row, hipMemcpyDeviceToHost), "kv read");
+    HIPCHK(hipMemcpy((char*)host_v + p * row, v, m * row, hipMemcpyDeviceToHost), "kv read");
+  }
   return MOA_OK;
 }
 

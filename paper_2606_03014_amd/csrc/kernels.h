@@ -216,8 +216,9 @@ struct AppendArgs {
 };
 // x_bf16: rows and q are bf16 (else f32).
 hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a);
+// row_pos null: positions pos0 .. pos0 + T; place.key null: sequence 0.
 hipError_t launch_kv_read(hipStream_t st, int kind, const void* kv, int layer, int n_kv, int hd, int T,
-                          const int* row_pos, const KvPlace& place, void* k, void* v);
+                          const int* row_pos, int pos0, const KvPlace& place, void* k, void* v);
 
 // Attention over 4-bit cells. Types of q and out: f32, bf16, or (out only) the
 // split-bf16 pair of the GEMM inputs, lo plane out_lo elements after hi.
@@ -241,8 +242,19 @@ struct Attend4Args {
 };
 hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace);
 hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* workspace);
+// The engine's work lists: items over splits of `split` keys (partials as launch_attn_reduce reads
+// them), and prefill blocks of at most kPrefillRows / (n_h / n_kv) rows; a.tables is the block store.
+hipError_t launch_attend4_items(hipStream_t st, const Attend4Args& a, const AttnItem* items, int nitems, int split,
+                                float* pacc, float* pml);
+hipError_t launch_attend4_prefill(hipStream_t st, const Attend4Args& a, const PrefillItem* items, int nitems);
 size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx);
 size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx);
+
+// Injected history into 4-bit cells (src: bf16; values as launch_kv_fill's, rounded to bf16).
+hipError_t launch_kv4_scatter(hipStream_t st, const void* src, void* kv, const int* blocks, int p0, int n, int layer,
+                              int kv_sel, int num_blocks, int n_kv, int hd);
+hipError_t launch_kv4_fill(hipStream_t st, void* kv, const int* bt_store, const FillReq* reqs, int nreqs, int nitems,
+                           int n_layers, int num_blocks, int n_kv, int hd);
 
 constexpr int kMaxTop = 32;
 struct ScoreArgs {
@@ -250,12 +262,13 @@ struct ScoreArgs {
   bool bf16;
   size_t stride;
   int rows, vocab, top;
-  const int* tokens;
+  const int *tokens, *token_at;   // row r's token: tokens[token_at ? token_at[r] : r]
   float *logprob, *entropy;
   int* top_ids;
   float* top_logprobs;
 };
 hipError_t launch_score(hipStream_t st, const ScoreArgs& a, void* workspace);
 size_t score_bytes(int rows, int vocab, int top);
+size_t score_bytes_max(int vocab);       // over all numbers of rows and alternatives
 
 }  // namespace moa

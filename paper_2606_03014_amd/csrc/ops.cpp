@@ -143,7 +143,7 @@ moa_status moa_kv_read(const moa_kv_cfg* c, const void* kv, int32_t layer, int32
   if (n_rows == 0) return MOA_OK;
   if (!aligned(row_seq, 4) || !aligned(row_pos, 4) || !aligned(k, 16) || !aligned(v, 16)) return MOA_EINVAL;
   return status_of(launch_kv_read((hipStream_t)hip_stream, c->kind, kv, layer, c->n_kv_heads, c->head_dim, n_rows,
-                                  row_pos, place_of(c, row_seq, tables, n_seqs, table_len), k, v), "moa_kv_read");
+                                  row_pos, 0, place_of(c, row_seq, tables, n_seqs, table_len), k, v), "moa_kv_read");
 }
 
 moa_status moa_kv_attend_bytes(const moa_kv_cfg* c, int32_t n_rows, int32_t max_ctx, size_t* bytes) {

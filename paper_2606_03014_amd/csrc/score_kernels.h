@@ -73,7 +73,7 @@ __device__ __forceinline__ void score_row(const ScoreArgs& a, int r, const Score
   const bool bad = s.sum != s.sum || !(fabsf(s.m) < INFINITY);    // NaN, +inf, or nothing above -inf
   const float nan = __uint_as_float(0x7fc00000u), norm = bad ? nan : logf(s.sum);
   if (tid == 0) {
-    const int tok = a.tokens[r];
+    const int tok = a.tokens[a.token_at ? a.token_at[r] : r];
     a.logprob[r] = (unsigned)tok < (unsigned)V ? at(tok) - s.m - norm : nan;
     a.entropy[r] = norm - s.mom / s.sum;
   }
@@ -292,6 +292,12 @@ size_t score_bytes(int rows, int vocab, int top) {
   int nseg, seg_steps;
   plan_score(rows, vocab, nseg, seg_steps);
   return nseg > 1 ? (size_t)rows * nseg * (sizeof(float4) + 8 * (size_t)top) : 0;
+}
+
+size_t score_bytes_max(int vocab) {
+  size_t most = 0;
+  for (int rows = 1; rows <= 512; ++rows) most = std::max(most, score_bytes(rows, vocab, kMaxTop));
+  return most;
 }
 
 hipError_t launch_score(hipStream_t st, const ScoreArgs& a, void* workspace) {

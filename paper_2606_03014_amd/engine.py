@@ -22,8 +22,10 @@ def model_cfg(shape):
 
 
 def engine_cfg(shape, dtype, consts, max_models, plan_only=False, token_store=0, block_store=0,
-               one_stream=False):
-    flags = (M.MOA_FLAG_PLAN_ONLY if plan_only else 0) | (M.MOA_FLAG_ONE_STREAM if one_stream else 0)
+               one_stream=False, kv_int4=False, qk_norm=False, scores=False):
+    flags = (M.MOA_FLAG_PLAN_ONLY if plan_only else 0) | (M.MOA_FLAG_ONE_STREAM if one_stream else 0) \
+        | (M.MOA_FLAG_KV_INT4 if kv_int4 else 0) | (M.MOA_FLAG_QK_NORM if qk_norm else 0) \
+        | (M.MOA_FLAG_SCORES if scores else 0)
     return M.moa_engine_cfg(model_cfg(shape), M.MOA_BF16 if dtype == "bf16" else M.MOA_F32,
                             consts.kv_block_size, consts.num_kv_blocks, consts.max_num_seqs,
                             consts.max_prefill_tokens, consts.max_model_len, max_models,
@@ -31,12 +33,17 @@ def engine_cfg(shape, dtype, consts, max_models, plan_only=False, token_store=0,
 
 
 class Engine:
-    """Owns one moa_engine and (unless plan_only) its torch-allocated arena."""
+    """Owns one moa_engine and (unless plan_only) its torch-allocated arena.
+
+    kv_int4: K and V cached in 4 bits (bf16 engines). qk_norm: models with per-head norms of queries and keys.
+    scores: request_scores() may be called."""
 
     def __init__(self, shape, dtype, consts, max_models, plan_only=False, device="cuda:0",
-                 token_store=0, block_store=0, one_stream=False):
+                 token_store=0, block_store=0, one_stream=False, kv_int4=False, qk_norm=False, scores=False):
         self.shape = shape
-        self.cfg = engine_cfg(shape, dtype, consts, max_models, plan_only, token_store, block_store, one_stream)
+        self.cfg = engine_cfg(shape, dtype, consts, max_models, plan_only, token_store, block_store, one_stream,
+                              kv_int4, qk_norm, scores)
+        self._scores = {}
         self.arena_bytes = M.moa_arena_bytes(self.cfg)
         self.plan_only = plan_only
         self.arena = None
@@ -67,7 +74,25 @@ class Engine:
         return M.moa_step_noalloc(self.h)
 
     def collect(self, upto=-1):
-        return M.moa_collect(self.h, upto)
+        done = M.moa_collect(self.h, upto)
+        for d in done:
+            self._scores.pop(d[0], None)       # the arrays are complete, and the caller's alone
+        return done
+
+    def request_scores(self, rid, top_k=0):
+        """Score the tokens that request rid emits: numpy arrays (logprob [G], entropy [G], top_ids [G, top_k],
+        top_logprobs [G, top_k]), complete once the request has been collected."""
+        G = self.request(rid).max_new_tokens
+        arrays = (np.full(G, np.nan, np.float32), np.full(G, np.nan, np.float32),
+                  np.full((G, top_k), -1, np.int32), np.full((G, top_k), np.nan, np.float32))
+        M.moa_request_scores(self.h, rid, *arrays[:2], *(arrays[2:] if top_k else ()))
+        self._scores[rid] = arrays             # the engine writes to them until then
+        return arrays
+
+    def kv(self, rid, layer, n):
+        """(k, v) of the first n cached positions of a running request."""
+        s = self.shape
+        return M.moa_debug_kv(self.h, rid, layer, n, s.n_kv_heads, s.head_dim, self.cfg.dtype == M.MOA_BF16)
 
     def sync(self):
         M.moa_sync(self.h)

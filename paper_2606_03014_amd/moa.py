@@ -14,6 +14,7 @@ MOA_OK, MOA_EINVAL, MOA_ENOMEM, MOA_ENOSPC, MOA_ESTATE, MOA_EHIP = 0, -1, -2, -3
 MOA_F32, MOA_BF16 = 0, 1
 MOA_FLAG_PLAN_ONLY = 1
 MOA_FLAG_ONE_STREAM = 2
+MOA_FLAG_KV_INT4, MOA_FLAG_QK_NORM, MOA_FLAG_SCORES = 4, 8, 16
 MOA_KV_F32, MOA_KV_BF16, MOA_KV_INT4 = 0, 1, 2
 MOA_MAX_TOP = 32
 STATUS_NAMES = {0: "MOA_OK", -1: "MOA_EINVAL", -2: "MOA_ENOMEM", -3: "MOA_ENOSPC",
@@ -81,6 +82,9 @@ _SIGS = {
     "moa_step_noalloc": (C.c_int, [C.c_void_p, P(moa_step_info)]),
     "moa_collect": (C.c_int, [C.c_void_p, C.c_int64, P(moa_result), C.c_int32, P(C.c_int32),
                               P(C.c_int32), C.c_int64]),
+    "moa_request_scores": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, P(C.c_float), P(C.c_float), P(C.c_int32),
+                                     P(C.c_float)]),
+    "moa_debug_kv": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
     "moa_sync": (C.c_int, [C.c_void_p]),
     "moa_destroy": (None, [C.c_void_p]),
     "moa_status_str": (C.c_char_p, [C.c_int]),
@@ -226,6 +230,29 @@ def moa_collect(eng, upto_step=-1):
         tok_cap *= 4
     return [(res[i].request_id, res[i].model_id, res[i].finish_step,
              buf[res[i].tok_offset: res[i].tok_offset + res[i].n_tokens].copy()) for i in range(n.value)]
+
+
+def moa_request_scores(eng, rid, logprob, entropy, top_ids=None, top_logprobs=None):
+    """Contiguous numpy arrays that the caller keeps until the request is collected: float32 [G], [G], int32 and float32
+    [G, top_k] (None: no alternatives)."""
+    import numpy as np
+    top_k = 0 if top_ids is None else top_ids.shape[1]
+    args = []
+    for a, t, c in ((logprob, np.float32, C.c_float), (entropy, np.float32, C.c_float), (top_ids, np.int32, C.c_int32),
+                    (top_logprobs, np.float32, C.c_float)):
+        if a is not None and (a.dtype != t or not a.flags.c_contiguous):
+            raise ValueError("score arrays must be contiguous float32 (ids: int32)")
+        args.append(None if a is None else a.ctypes.data_as(P(c)))
+    check(lib().moa_request_scores(eng, rid, top_k, *args), "moa_request_scores")
+
+
+def moa_debug_kv(eng, rid, layer, n, n_kv_heads, head_dim, bf16):
+    """(k, v) of positions [0, n): uint16 bf16 bits or float32 [n, n_kv_heads, head_dim]."""
+    import numpy as np
+    k = np.zeros((n, n_kv_heads, head_dim), dtype=np.uint16 if bf16 else np.float32)
+    v = np.zeros_like(k)
+    check(lib().moa_debug_kv(eng, rid, layer, n, k.ctypes.data_as(C.c_void_p), v.ctypes.data_as(C.c_void_p)), "moa_debug_kv")
+    return k, v
 
 
 def moa_sync(eng):
