@@ -15,27 +15,30 @@ import numpy as np
 
 LAYER_TENSORS = ("attn_norm", "wq", "wk", "wv", "wo",
                  "mlp_norm", "w_gate", "w_up", "w_down")
+# models with norms of queries and keys for each head
+QK_LAYER_TENSORS = LAYER_TENSORS[:4] + ("q_norm", "k_norm") + LAYER_TENSORS[4:]
 
 
-def TENSOR_NAMES(n_layers):
+def TENSOR_NAMES(n_layers, qk_norm=False):
     names = ["embed"]
     for l in range(n_layers):
-        names += [f"layers.{l}.{t}" for t in LAYER_TENSORS]
+        names += [f"layers.{l}.{t}" for t in (QK_LAYER_TENSORS if qk_norm else LAYER_TENSORS)]
     names += ["final_norm", "lm_head"]
     return names
 
 
-def tensor_shapes(m):
+def tensor_shapes(m, qk_norm=False):
     """(name, shape) in blob order for a ModelShape ``m``."""
     d, hd = m.d_model, m.head_dim
     per = {
         "attn_norm": (d,), "wq": (m.n_heads * hd, d), "wk": (m.n_kv_heads * hd, d),
         "wv": (m.n_kv_heads * hd, d), "wo": (d, m.n_heads * hd), "mlp_norm": (d,),
         "w_gate": (m.ffn_dim, d), "w_up": (m.ffn_dim, d), "w_down": (d, m.ffn_dim),
+        "q_norm": (hd,), "k_norm": (hd,),
     }
     out = [("embed", (m.vocab, d))]
     for l in range(m.n_layers):
-        out += [(f"layers.{l}.{t}", per[t]) for t in LAYER_TENSORS]
+        out += [(f"layers.{l}.{t}", per[t]) for t in (QK_LAYER_TENSORS if qk_norm else LAYER_TENSORS)]
     out += [("final_norm", (d,)), ("lm_head", (m.vocab, d))]
     return out
 
@@ -63,19 +66,19 @@ def _draw(seed, wid, model_id, idx, name, shape, dtype):
     return a
 
 
-def generate_weights(model_shape, dtype, seed, wid, model_id, n_layers=None, threads=8):
+def generate_weights(model_shape, dtype, seed, wid, model_id, n_layers=None, threads=8, qk_norm=False):
     """Dict name -> array (float32, or uint16 bf16 bits). ``n_layers`` may
     truncate the depth (same streams for the layers that remain)."""
     m = model_shape
-    shapes = tensor_shapes(m)
+    shapes = tensor_shapes(m, qk_norm)
     if n_layers is not None and n_layers != m.n_layers:
         from dataclasses import replace
         m2 = replace(m, n_layers=n_layers)
-        keep = {n for n, _ in tensor_shapes(m2)}
+        keep = {n for n, _ in tensor_shapes(m2, qk_norm)}
         # final_norm / lm_head keep their full-depth tensor index so the head
         # is the same matrix whatever the depth.
         shapes = [(n, s) for n, s in shapes if n in keep]
-    index = {n: i for i, (n, _) in enumerate(tensor_shapes(m))}
+    index = {n: i for i, (n, _) in enumerate(tensor_shapes(m, qk_norm))}
     with ThreadPoolExecutor(max_workers=threads) as ex:
         futs = {n: ex.submit(_draw, seed, wid, model_id, index[n], n, s, dtype)
                 for n, s in shapes}
@@ -86,5 +89,6 @@ def pack_blob(weights, model_shape, n_layers=None):
     """Concatenate tensors in blob order into one contiguous numpy byte array."""
     from dataclasses import replace
     m = model_shape if n_layers is None else replace(model_shape, n_layers=n_layers)
-    parts = [weights[n].reshape(-1).view(np.uint8) for n, _ in tensor_shapes(m)]
+    shapes = tensor_shapes(m, "layers.0.q_norm" in weights)
+    parts = [weights[n].reshape(-1).view(np.uint8) for n, _ in shapes]
     return np.concatenate(parts)

@@ -26,6 +26,11 @@ All arithmetic is float64 (weights are upcast from their fp32 or bf16
 storage). ``bf16_kv=True`` models a model state whose KV cache is stored in
 bf16: k (after RoPE) and v are rounded to bf16 (nearest-even) when they are
 written to the cache, exactly once; everything else stays float64.
+``int4_kv=True`` does the same for a cache in 4 bits: every (position, KV head)
+row of k and of v becomes what its 16 levels stand for (int4_round).
+
+A model whose weights hold q_norm and k_norm normalises the queries and the keys
+of each head, n() over the head, before the rotation.
 
 Parity pins (tests/test_oracle_*.py): single-key attention returns V, equal
 keys average V, softmax rows sum to 1, the blockwise causal attention of a
@@ -48,6 +53,16 @@ def bf16_round(a):
     r = ((u >> 16) & 1) + np.uint32(0x7FFF)
     out = ((u + r) & np.uint32(0xFFFF0000)).view(np.float32)
     return out.astype(np.float64)
+
+
+def int4_round(a):
+    """What rows (last axis) of a 4-bit cache stand for: m + s c with m = bf16(min), s = bf16((max - min) / 15) and
+    c = (x - m) / s rounded half to even, clamped to 0 .. 15; x is the float32 value."""
+    x = np.ascontiguousarray(a, dtype=np.float32)
+    lo, hi = x.min(axis=-1, keepdims=True), x.max(axis=-1, keepdims=True)
+    m, s = bf16_round(lo), bf16_round((hi - lo) / np.float32(15))
+    c = np.clip(np.rint((x.astype(np.float64) - m) / np.where(s > 0, s, 1.0)), 0, 15)
+    return m + s * np.where(s > 0, c, 0.0)
 
 
 def to_f64(arr):
@@ -203,7 +218,7 @@ class PagedKV:
         return K, V
 
 
-def forward_chunk(model, tokens, start, kv, bf16_kv=False, want="all"):
+def forward_chunk(model, tokens, start, kv, bf16_kv=False, want="all", int4_kv=False):
     """Run positions [start, start + len(tokens)) through the model, appending
     their K/V to ``kv`` (whose first ``start`` positions must already hold the
     history). Each position attends causally to positions <= itself.
@@ -211,7 +226,7 @@ def forward_chunk(model, tokens, start, kv, bf16_kv=False, want="all"):
     row, an integer ``want=j`` only rows j.. (the others are not computed)."""
     m = model.shape
     n_h, n_kv, hd = m.n_heads, m.n_kv_heads, m.head_dim
-    store = bf16_round if bf16_kv else (lambda a: a)
+    store = int4_round if int4_kv else (bf16_round if bf16_kv else (lambda a: a))
     toks = np.asarray(tokens, dtype=np.int64)
     T = toks.shape[0]
     pos = np.arange(start, start + T)
@@ -224,6 +239,9 @@ def forward_chunk(model, tokens, start, kv, bf16_kv=False, want="all"):
         q = (xn @ model.W(p + "wq").T).reshape(T, n_h, hd)
         k = (xn @ model.W(p + "wk").T).reshape(T, n_kv, hd)
         v = (xn @ model.W(p + "wv").T).reshape(T, n_kv, hd)
+        if p + "q_norm" in model.w:
+            q = rmsnorm(q, model.W(p + "q_norm"), m.rms_eps)
+            k = rmsnorm(k, model.W(p + "k_norm"), m.rms_eps)
         q = apply_rope(q, cos, sin)
         k = store(apply_rope(k, cos, sin))
         v = store(v)
@@ -244,10 +262,10 @@ def forward_chunk(model, tokens, start, kv, bf16_kv=False, want="all"):
     return xf @ model.W("lm_head").T
 
 
-def forward_full(model, tokens, bf16_kv=False, first=0):
+def forward_full(model, tokens, bf16_kv=False, first=0, int4_kv=False):
     """Logits at positions first.. of ``tokens`` computed from scratch (no prior cache)."""
     kv = ContiguousKV(model.n_layers, model.shape.n_kv_heads, model.shape.head_dim)
-    return forward_chunk(model, tokens, 0, kv, bf16_kv, want=first)
+    return forward_chunk(model, tokens, 0, kv, bf16_kv, want=first, int4_kv=int4_kv)
 
 
 def brute_force_prefix_logits(model, tokens, bf16_kv=False):
@@ -275,16 +293,16 @@ def greedy_generate(model, prompt, G, kv=None, bf16_kv=False, return_logits=Fals
     return out
 
 
-def teacher_forced_logits(model, prompt, outputs, bf16_kv=False):
+def teacher_forced_logits(model, prompt, outputs, bf16_kv=False, int4_kv=False):
     """Logits that produce each of ``outputs`` when the history is the prompt
     followed by the given outputs (so a flip never cascades): rows are the
     positions P-1 .. P+G-2 of prompt ++ outputs[:-1]."""
     seq = np.concatenate([np.asarray(prompt, dtype=np.int64),
                           np.asarray(outputs[:-1], dtype=np.int64)])
-    return forward_full(model, seq, bf16_kv, first=len(prompt) - 1)
+    return forward_full(model, seq, bf16_kv, first=len(prompt) - 1, int4_kv=int4_kv)
 
 
-def decode_from_history(model, K_hist, V_hist, token, pos, bf16_kv=False):
+def decode_from_history(model, K_hist, V_hist, token, pos, bf16_kv=False, int4_kv=False):
     """One decode step for a sequence whose K/V at positions [0, pos) is given
     (per layer [pos, n_kv, hd]); returns the logits of ``token`` at ``pos``."""
     m = model.shape
@@ -292,4 +310,4 @@ def decode_from_history(model, K_hist, V_hist, token, pos, bf16_kv=False):
     for l in range(model.n_layers):
         kv.K[l] = np.asarray(K_hist[l], dtype=np.float64)
         kv.V[l] = np.asarray(V_hist[l], dtype=np.float64)
-    return forward_chunk(model, [token], pos, kv, bf16_kv)[-1]
+    return forward_chunk(model, [token], pos, kv, bf16_kv, int4_kv=int4_kv)[-1]
