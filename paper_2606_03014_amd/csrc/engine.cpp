@@ -1102,14 +1102,13 @@ size_t noalloc_scratch_bytes(const moa_engine* e) {
 
 moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int T, int R,
                         const int* grp_rows, const int* grp_lm, bool noalloc,
-                        std::vector<moa_engine::Score>& score_rows) {
+                        std::vector<moa_engine::Score>& want) {
   const moa_model_cfg& g = e->cfg.model;
   const Layout& L = e->lay;
   const int slot = (int)(e->step_idx % kStageSlots);
   moa_status st = wait_slot(e, slot);
   if (st != MOA_OK) return st;
   e->keepalive[slot].clear();                 // the step that read them has completed
-  e->score_rows[slot].swap(score_rows);
 
   // partial sums: the arena's workspace, or this GPU's library scratch
   float* part = e->part;
@@ -1560,7 +1559,6 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     }
     // Token scores of the rows that ask for them, in runs of neighbouring rows (one
     // run over the rows between where there would be many), and one copy to the host.
-    std::vector<moa_engine::Score>& want = e->score_rows[slot];
     if (!want.empty()) {
       int k = 0;
       for (const moa_engine::Score& w : want) k = std::max(k, e->reqs[w.id].top);
@@ -1593,6 +1591,7 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
       }
       HIPCHK(hipMemcpyAsync(e->score_host[slot], e->scores, (size_t)R * (2 + 2 * k) * 4, hipMemcpyDeviceToHost, s),
              "score download");
+      e->score_rows[slot].swap(want);
     }
   }
   (void)L;

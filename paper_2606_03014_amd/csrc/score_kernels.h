@@ -80,7 +80,7 @@ __device__ __forceinline__ void score_row(const ScoreArgs& a, int r, const Score
   if (k == 0) return;
   int* ids = a.top_ids + (size_t)r * k;
   float* tops = a.top_logprobs + (size_t)r * k;
-  if (!over && (n >= k || s.sum == s.sum || s.m == -INFINITY)) {
+  if (!over && (n >= k || s.sum == s.sum)) {
     rank_keys(keys, n, k, [&](int rk, u64 key) {
       ids[rk] = (int)~(unsigned)key;
       tops[rk] = bad ? nan : key_value(key) - s.m - norm;
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(1024, 8) void k_score(ScoreArgs a, int nseg, int se
   float bar = INFINITY;
   int cur = 0;
   bool over = false;                                     // the list did not hold a step's candidates
-  if (tid == 0) cnt = 0;
+  if (tid == 0) { cnt = 0; sbar = ninf; }               // fewer than k groups that are not NaN: no bar
   load(c0);
   for (int c = c0; c < c1; ++c) {
     float x[16];
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(1024, 8) void k_score(ScoreArgs a, int nseg, int se
         int rk = 0;
 #pragma unroll
         for (int j = part; j < 64; j += 16) rk += gm[j] > g || (gm[j] == g && j < i);
-        if ((int)sum16((float)rk) == k - 1) sbar = g;
+        if ((int)sum16((float)rk) == k - 1 && g == g) sbar = g;
         __syncthreads();
         bar = sbar;
       }

@@ -605,6 +605,27 @@ def test_rows_without_probabilities_and_tokens_outside(ops, V):
     assert torch.equal(ids[1].cpu(), torch.sort(rest, descending=True, stable=True)[1][:6].int())
 
 
+@gpu
+@pytest.mark.parametrize("V", [300, 70000])
+def test_alternatives_of_rows_of_nan(ops, V):
+    """NaN everywhere, beside impossible tokens, and in all but three of the 64 groups that set the bar of a row's first run."""
+    x = torch.randn(4, V, generator=torch.Generator().manual_seed(5))
+    x[0] = math.nan
+    x[1] = math.nan
+    x[1, 2::9] = -math.inf
+    e = torch.arange(V)
+    x[2, (e < 16384) & (e // 4 % 64 >= 3)] = math.nan
+    x[3, 1:] = math.nan
+    lp, H, ids, tops = ops.score_tokens(x.cuda(), i32([0, 1, 2, 3]), top_k=20)
+    assert lp.isnan().all() and H.isnan().all() and tops.isnan().all()
+    for r in range(4):
+        v = x[r].numpy()
+        want = np.lexsort((np.arange(V), -np.nan_to_num(v, nan=0.0, neginf=-np.inf), np.isnan(v)))[:20]
+        assert ids[r].tolist() == want.tolist(), r
+    one = ops.score_tokens(x.cuda(), i32([0, 1, 2, 3]), top_k=1)[2][:, 0].tolist()
+    assert one == ids[:, 0].tolist()
+
+
 # ------------------------------------------------------------------ together, streams and graphs
 
 class Session:
