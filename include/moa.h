@@ -376,7 +376,11 @@ moa_status moa_debug_measure_peaks(moa_engine* e, double* read_bytes_per_s, doub
  * nothing is allocated, copied to the host or waited for, so the calls can be
  * captured into a graph. Matrices are row-major; a stride is the elements
  * from one row to the next (at least the row's width, any alignment of the
- * element). Sizes and the values of cfg are checked (MOA_EINVAL); index
+ * element). No output may overlap an input or another output. Sizes and the
+ * values of cfg are checked (MOA_EINVAL): at most 2^20 rows, sequences and
+ * chunks, 2^26 entries a table row, 2^30 tokens, and for attention fewer than
+ * 2^24 workgroups (KV heads times rows, or blocks of 128 queries, times
+ * splits of the keys). Index
  * tensors are read on the device, where an entry that is out of range is
  * skipped as each call states. A call of zero rows does nothing. workspace
  * (256-byte aligned, MOA_ENOMEM if it is smaller than the *_bytes call says)
@@ -396,10 +400,12 @@ enum { MOA_KV_F32 = 0, MOA_KV_BF16 = 1, MOA_KV_INT4 = 2 };
  *     V codes [D / 2][16]: byte i of a position has dims i (low four bits) and i + D / 2;
  *     K scales [16], V scales [16]: bf16 pairs (s, m), s in the lower half of the word.
  *   Code c stands for m + s c. A row (a position's K or V of one head, as
- *   float32) is stored with m = bf16(min), s = bf16((max - min) / 15) and
+ *   float32) is stored with m = bf16(min), s = bf16((max - min) * (1 / 15)),
+ *   1 / 15 and the product in float32, and
  *   c = (x - m) / s rounded half to even and clamped to 0 .. 15 (0 where s = 0).
  *   A row with a NaN, an infinity or a range past float32 has s = NaN, so all
- *   of it stands for NaN. */
+ *   of it stands for NaN. Attention sums s c with factors up to 2^24: values
+ *   from 2^100 on may become infinite there. */
 typedef struct {
   int32_t kind, n_layers, num_blocks, n_heads, n_kv_heads, head_dim;
 } moa_kv_cfg;

@@ -56,11 +56,11 @@ def bf16_round(a):
 
 
 def int4_round(a):
-    """What rows (last axis) of a 4-bit cache stand for: m + s c with m = bf16(min), s = bf16((max - min) / 15) and
-    c = (x - m) / s rounded half to even, clamped to 0 .. 15; x is the float32 value."""
+    """What rows (last axis) of a 4-bit cache stand for: m + s c with m = bf16(min), s = bf16((max - min) * (1 / 15)) (in
+    float32) and c = (x - m) / s rounded half to even, clamped to 0 .. 15; x is the float32 value."""
     x = np.ascontiguousarray(a, dtype=np.float32)
     lo, hi = x.min(axis=-1, keepdims=True), x.max(axis=-1, keepdims=True)
-    m, s = bf16_round(lo), bf16_round((hi - lo) / np.float32(15))
+    m, s = bf16_round(lo), bf16_round((hi - lo) * np.float32(1 / 15))
     c = np.clip(np.rint((x.astype(np.float64) - m) / np.where(s > 0, s, 1.0)), 0, 15)
     return m + s * np.where(s > 0, c, 0.0)
 

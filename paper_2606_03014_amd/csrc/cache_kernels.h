@@ -34,9 +34,10 @@ __device__ __forceinline__ T over_row(T v, F f) {
 
 // One 4-bit row from hd / N lanes, lane l holding dims N / 2 l .. + N / 2 and the
 // same + hd / 2: its scale word and the lane's N codes.
-// The quotient is formed in 64 bits from the exact difference and rounded to 24
-// before the rounding to a code, so a quotient that lies on the border of two codes
-// (bf16 values often do) is a tie here too, and goes to the even code.
+// The quotient is that of 64-bit division (a product with the reciprocal, and one step
+// that takes its residual in): exact where it lies on the border of two codes, as bf16
+// values often do, and on the right side of it otherwise. Rounded to 24 bits it made a
+// tie, and the other code, of one float32 value in a million.
 template <int HD, int N>
 __device__ __forceinline__ unsigned quantise(const float x[N], int c[N]) {
   constexpr int LP = HD / N;
@@ -48,14 +49,18 @@ __device__ __forceinline__ unsigned quantise(const float x[N], int c[N]) {
   for (int i = 1; i < N; ++i) { lo = least(lo, x[i]); hi = most(hi, x[i]); }
   lo = over_row<LP>(lo, least);
   hi = over_row<LP>(hi, most);
-  unsigned word = pack_bf16((hi - lo) / 15.f, lo);
+  unsigned word = pack_bf16((hi - lo) * (1.f / 15.f), lo);   // a product: a division is ten instructions, and no better a step
   if (!(hi - lo < INFINITY) || !(fabsf(__uint_as_float(word & 0xffff0000u)) < INFINITY)) word = 0x7fc0u;
   const float sf = __uint_as_float(word << 16);
-  // 2^-40 of the reciprocal is enough: the quotient is rounded to 24 bits
-  const double md = __uint_as_float(word & 0xffff0000u), sd = sf > 0.f ? (double)sf : 1.0, r = __builtin_amdgcn_rcp(sd);
-  const double inv = sf > 0.f ? r * (2.0 - sd * r) : 0.0;
+  const bool some = sf > 0.f;                            // else all codes are 0, for NaN too
+  const double md = __uint_as_float(word & 0xffff0000u), sd = some ? (double)sf : 1.0;
+  double inv = __builtin_amdgcn_rcp(sd);                 // 2^-24; after the step 2^-48, which the residual squares
+  inv = fma(inv, fma(-sd, inv, 1.0), inv);
 #pragma unroll
-  for (int i = 0; i < N; ++i) c[i] = (int)fminf(fmaxf(rintf((float)(((double)x[i] - md) * inv)), 0.f), 15.f);   // inv = 0: 0, for NaN too
+  for (int i = 0; i < N; ++i) {
+    const double d = (double)x[i] - md, u = d * inv, q = fma(fma(-sd, u, d), inv, u);
+    c[i] = some ? (int)__builtin_rint(fmin(fmax(q, 0.0), 15.0)) : 0;
+  }
   return word;
 }
 
@@ -411,6 +416,18 @@ struct Partial4 { float *acc, *ml; };              // [slot][n_h][hd] sums; [slo
 __device__ __forceinline__ unsigned pack_f16(float a, float b) {
   return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
 }
+// For a head whose largest |q| is mx: the power of two, with scale's sign, that brings q just below
+// 2^13, and a score's unit after it in powers of two (f > 0). The exponent stops at 2^-100,
+// so that the factor of subnormal queries stays finite; a scale that leaves no unit is 0.
+__device__ __forceinline__ void q_units(float mx, float scale, float& up, float& f) {
+  int e = 0;
+  if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
+  e = max(e, -100);
+  f = ldexpf(fabsf(scale) * 1.4426950408889634f, e - 13);
+  const bool some = f > 0.f;
+  up = some ? copysignf(ldexpf(1.f, 13 - e), scale) : 0.f;
+  f = some ? f : 1.f;
+}
 // Over a column of four lanes 16 apart.
 __device__ __forceinline__ float max_column(float v) {
   v = fmaxf(v, swz_xor16(v));
@@ -526,9 +543,8 @@ __global__ __launch_bounds__(256, 3) void k_attend4_rows(Attend4Args a, const At
       float mx = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
       mx = max16(mx);
       if constexpr (TH == 32) mx = fmaxf(mx, swz_xor16(mx));
-      int e = 0;
-      if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
-      const float up = a.scale > 0.f ? ldexpf(1.f, 13 - e) : (a.scale < 0.f ? -ldexpf(1.f, 13 - e) : 0.f);
+      float up, f;
+      q_units(mx, a.scale, up, f);
       float sum = 0.f;
       uint16_t* hi = (uint16_t*)sq[(d >> 3) % W][17 * ((d >> 3) / W) + h] + ((d >> 2) & 1);
 #pragma unroll
@@ -544,8 +560,7 @@ __global__ __launch_bounds__(256, 3) void k_attend4_rows(Attend4Args a, const At
       if constexpr (TH == 32) sum += swz_xor16(sum);
       if (threadIdx.x % TH == 0) {
         sqf[0][h] = sum;
-        const float f = ldexpf(fabsf(a.scale) * 1.4426950408889634f, e - 13);
-        sqf[1][h] = f > 0.f ? f : 1.f;
+        sqf[1][h] = f;
       }
     }
   }
@@ -751,7 +766,7 @@ __device__ __forceinline__ Chunk find_chunk(const Attend4Args& a, int b, int PB)
   const int s0 = max(a.chunk_start[i], 0), s1 = min(a.chunk_start[i + 1], a.T);
   const int r0 = s0 + (b - (s0 / PB + i)) * PB;
   c.row0 = r0;
-  c.nq = max(min(PB, s1 - r0), 0);
+  c.nq = r0 < s0 ? 0 : max(min(PB, s1 - r0), 0);   // r0 < s0: the starts do not ascend
   c.pos0 = min(a.chunk_ctx[i], a.max_ctx) - (s1 - r0);
   c.tab = a.tables + (size_t)i * a.table_len;
   return c;
@@ -889,11 +904,8 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
       for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[s][i]));
     }
     mx = max_halves(mx);
-    int e = 0;
-    if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
-    const float up = a.scale > 0.f ? ldexpf(1.f, 13 - e) : (a.scale < 0.f ? -ldexpf(1.f, 13 - e) : 0.f);
-    f = ldexpf(fabsf(a.scale) * 1.4426950408889634f, e - 13);
-    if (!(f > 0.f)) f = 1.f;
+    float up;
+    q_units(mx, a.scale, up, f);
     float sum = 0.f;
 #pragma unroll
     for (int s = 0; s < DS; ++s)
@@ -1082,6 +1094,8 @@ __global__ __launch_bounds__(256) void k_attend4_chunks_join(Attend4Args a, int 
 
 // =============================================================== launchers
 
+constexpr long long kMaxGrid = (1ll << 24) - 1;    // workgroups of 256 in a grid: its threads are counted in 32 bits
+
 hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& args) {
   if (args.T <= 0) return hipSuccess;
   AppendArgs a = args;
@@ -1143,6 +1157,11 @@ static int split4(int n_kv, int T, int max_ctx) {
 }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+bool attend4_rows_fits(int n_kv, int T, int max_ctx) {
+  const int s = split4(n_kv, T, max_ctx);
+  return (long long)T * ((max_ctx + s - 1) / s) * n_kv <= kMaxGrid;
+}
+
 size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx) {
   const int s = split4(n_kv, T, max_ctx), n = (max_ctx + s - 1) / s;
   const size_t slots = n > 1 ? (size_t)T * n : 0;
@@ -1152,7 +1171,7 @@ size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx) {
 hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* workspace) {
   if (a.T <= 0) return hipSuccess;
   const int s = split4(a.n_kv, a.T, a.max_ctx), n = (a.max_ctx + s - 1) / s;
-  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)a.T * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)a.T * n * a.n_kv > kMaxGrid) return hipErrorInvalidValue;
   Partial4 part{(float*)workspace, (float*)((char*)workspace + up256((size_t)a.T * n * a.n_h * a.hd * 4))};
   const dim3 grid((unsigned)(a.T * n * a.n_kv)), blk(256);
   const bool vec = a.q_stride % (a.q_bf16 ? 8 : 4) == 0 && (uintptr_t)a.q % 16 == 0;
@@ -1176,6 +1195,12 @@ static void plan_chunks4(int n_h, int n_kv, int T, int n_chunks, int max_ctx, in
   nsplit = (max_ctx + split - 1) / split;
 }
 
+bool attend4_chunks_fits(int n_h, int n_kv, int T, int n_chunks, int max_ctx) {
+  int nslots, split, n;
+  plan_chunks4(n_h, n_kv, T, n_chunks, max_ctx, nslots, split, n);
+  return (long long)nslots * n * n_kv <= kMaxGrid;
+}
+
 size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx) {
   int nslots, split, n;
   plan_chunks4(n_h, n_kv, T, n_chunks, max_ctx, nslots, split, n);
@@ -1184,15 +1209,19 @@ size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int 
 
 static unsigned chunks4_lds(int hd) { return 4u * 64u * (unsigned)hd * 2u + 3u * 1024u; }
 static hipError_t chunks4_attributes() {
-  static bool attr = false;                // one attribute call per process for the instantiations
-  if (attr) return hipSuccess;
+  static std::atomic<unsigned long long> done{0};    // devices whose instantiations have the attribute
+  int dev = 0;
+  const hipError_t err = hipGetDevice(&dev);
+  if (err != hipSuccess) return err;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (done.load() & bit) return hipSuccess;
   for (const void* f : {(const void*)k_attend4_chunks<64, false, false>, (const void*)k_attend4_chunks<64, false, true>,
                         (const void*)k_attend4_chunks<64, true, true>, (const void*)k_attend4_chunks<128, false, false>,
                         (const void*)k_attend4_chunks<128, false, true>, (const void*)k_attend4_chunks<128, true, true>}) {
     const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)chunks4_lds(128));
     if (e != hipSuccess) return e;
   }
-  attr = true;
+  done.fetch_or(bit);
   return hipSuccess;
 }
 
@@ -1200,7 +1229,7 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
   if (a.T <= 0) return hipSuccess;
   int nslots, split, n;
   plan_chunks4(a.n_h, a.n_kv, a.T, a.n_seqs, a.max_ctx, nslots, split, n);
-  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)nslots * n * a.n_kv > INT_MAX) return hipErrorInvalidValue;
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)nslots * n * a.n_kv > kMaxGrid) return hipErrorInvalidValue;
   Partial4 part{nullptr, nullptr};
   if (n > 1) part = {(float*)workspace, (float*)((char*)workspace + up256((size_t)n * a.T * a.n_h * a.hd * 4))};
   const unsigned shm = chunks4_lds(a.hd);
@@ -1221,7 +1250,7 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
 hipError_t launch_attend4_items(hipStream_t st, const Attend4Args& a, const AttnItem* items, int nitems, int split,
                                 float* pacc, float* pml) {
   if (nitems <= 0) return hipSuccess;
-  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || a.q_bf16 || split > kSplit4Max || (long long)nitems * a.n_kv > INT_MAX)
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || a.q_bf16 || split > kSplit4Max || (long long)nitems * a.n_kv > kMaxGrid)
     return hipErrorInvalidValue;
   const dim3 grid((unsigned)nitems * a.n_kv), blk(256);
   const Partial4 part{pacc, pml};
@@ -1232,7 +1261,7 @@ hipError_t launch_attend4_items(hipStream_t st, const Attend4Args& a, const Attn
 
 hipError_t launch_attend4_prefill(hipStream_t st, const Attend4Args& a, const PrefillItem* items, int nitems) {
   if (nitems <= 0) return hipSuccess;
-  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || a.q_bf16 || (long long)nitems * a.n_kv > INT_MAX)
+  if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || a.q_bf16 || (long long)nitems * a.n_kv > kMaxGrid)
     return hipErrorInvalidValue;
   const hipError_t e = chunks4_attributes();
   if (e != hipSuccess) return e;

@@ -247,6 +247,9 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
 hipError_t launch_attend4_items(hipStream_t st, const Attend4Args& a, const AttnItem* items, int nitems, int split,
                                 float* pacc, float* pml);
 hipError_t launch_attend4_prefill(hipStream_t st, const Attend4Args& a, const PrefillItem* items, int nitems);
+// (fits: the call's grid can be launched)
+bool attend4_rows_fits(int n_kv, int T, int max_ctx);
+bool attend4_chunks_fits(int n_h, int n_kv, int T, int n_chunks, int max_ctx);
 size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx);
 size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx);
 

@@ -10,6 +10,7 @@
 
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
+#include <atomic>
 #include <climits>
 #include <cmath>
 #include <mutex>

@@ -24,7 +24,16 @@ bool valid_kv(const moa_kv_cfg* c) {
   if (c->n_heads % c->n_kv_heads) return false;
   const int gq = c->n_heads / c->n_kv_heads;
   // a row's heads are one grid dimension, and their elements an int
-  return (gq == 1 || gq == 2 || gq == 4 || gq == 8) && c->n_heads <= 4096;
+  if ((gq != 1 && gq != 2 && gq != 4 && gq != 8) || c->n_heads > 4096) return false;
+  const double bytes = (double)c->n_layers * c->num_blocks * c->n_kv_heads * kv_cell_bytes(c->kind, c->head_dim);
+  return bytes < 0x1p60;                         // no size or offset overflows
+}
+
+// Counts of rows and sequences, table entries and tokens: grids and positions fit 32 bits.
+constexpr int32_t kMaxRows = 1 << 20, kMaxTable = 1 << 26, kMaxVocab = 1 << 30;
+
+size_t pool_bytes(const moa_kv_cfg* c) {
+  return (size_t)c->n_layers * c->num_blocks * c->n_kv_heads * kv_cell_bytes(c->kind, c->head_dim);
 }
 
 bool valid_type(int32_t t) { return t == MOA_F32 || t == MOA_BF16; }
@@ -33,8 +42,8 @@ bool aligned(const void* p, size_t a) { return p && (uintptr_t)p % a == 0; }
 // The pool, the layer, the rows and their tables of one call.
 bool valid_call(const moa_kv_cfg* c, const void* kv, int32_t layer, int32_t n_rows, const int32_t* tables,
                 int32_t n_seqs, int32_t table_len) {
-  return valid_kv(c) && aligned(kv, 16) && layer >= 0 && layer < c->n_layers && n_rows >= 0 && aligned(tables, 4) &&
-         n_seqs >= 1 && table_len >= 1 && table_len <= (1 << 26);
+  return valid_kv(c) && aligned(kv, 16) && layer >= 0 && layer < c->n_layers && n_rows >= 0 && n_rows <= kMaxRows &&
+         aligned(tables, 4) && n_seqs >= 1 && n_seqs <= kMaxRows && table_len >= 1 && table_len <= kMaxTable;
 }
 
 KvPlace place_of(const moa_kv_cfg* c, const int32_t* row_seq, const int32_t* tables, int32_t n_seqs, int32_t table_len) {
@@ -95,7 +104,7 @@ extern "C" {
 
 moa_status moa_kv_bytes(const moa_kv_cfg* c, size_t* bytes) {
   if (!valid_kv(c) || !bytes) return MOA_EINVAL;
-  *bytes = (size_t)c->n_layers * c->num_blocks * c->n_kv_heads * kv_cell_bytes(c->kind, c->head_dim);
+  *bytes = pool_bytes(c);
   return MOA_OK;
 }
 
@@ -147,7 +156,9 @@ moa_status moa_kv_read(const moa_kv_cfg* c, const void* kv, int32_t layer, int32
 }
 
 moa_status moa_kv_attend_bytes(const moa_kv_cfg* c, int32_t n_rows, int32_t max_ctx, size_t* bytes) {
-  if (!valid_kv(c) || c->kind != MOA_KV_INT4 || n_rows < 0 || max_ctx < 1 || !bytes) return MOA_EINVAL;
+  if (!valid_kv(c) || c->kind != MOA_KV_INT4 || n_rows < 0 || n_rows > kMaxRows || max_ctx < 1 || max_ctx > 16 * kMaxTable || !bytes)
+    return MOA_EINVAL;
+  if (!attend4_rows_fits(c->n_kv_heads, n_rows, max_ctx)) return MOA_EINVAL;
   *bytes = attend4_rows_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, max_ctx);
   return MOA_OK;
 }
@@ -160,7 +171,9 @@ moa_status moa_kv_attend(const moa_kv_cfg* c, const void* kv, int32_t layer, con
   if (st != MOA_OK) return st;
   if (n_rows == 0) return MOA_OK;
   if (!aligned(row_seq, 4) || !aligned(row_ctx, 4)) return MOA_EINVAL;
-  st = check_workspace(workspace, workspace_bytes, attend4_rows_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, max_ctx));
+  size_t need = 0;
+  st = moa_kv_attend_bytes(c, n_rows, max_ctx, &need);
+  if (st == MOA_OK) st = check_workspace(workspace, workspace_bytes, need);
   if (st != MOA_OK) return st;
   Attend4Args a = attend_args(c, kv, layer, q, type, q_stride, n_rows, tables, n_seqs, table_len, max_ctx, scale, out);
   a.row_seq = row_seq;
@@ -170,7 +183,10 @@ moa_status moa_kv_attend(const moa_kv_cfg* c, const void* kv, int32_t layer, con
 
 moa_status moa_kv_attend_chunks_bytes(const moa_kv_cfg* c, int32_t n_rows, int32_t n_chunks, int32_t max_ctx,
                                       size_t* bytes) {
-  if (!valid_kv(c) || c->kind != MOA_KV_INT4 || n_rows < 0 || n_chunks < 1 || max_ctx < 1 || !bytes) return MOA_EINVAL;
+  if (!valid_kv(c) || c->kind != MOA_KV_INT4 || n_rows < 0 || n_rows > kMaxRows || n_chunks < 1 || n_chunks > kMaxRows ||
+      max_ctx < 1 || max_ctx > 16 * kMaxTable || !bytes)
+    return MOA_EINVAL;
+  if (!attend4_chunks_fits(c->n_heads, c->n_kv_heads, n_rows, n_chunks, max_ctx)) return MOA_EINVAL;
   *bytes = attend4_chunks_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, n_chunks, max_ctx);
   return MOA_OK;
 }
@@ -184,8 +200,9 @@ moa_status moa_kv_attend_chunks(const moa_kv_cfg* c, const void* kv, int32_t lay
   if (st != MOA_OK) return st;
   if (n_rows == 0) return MOA_OK;
   if (!aligned(chunk_start, 4) || !aligned(chunk_ctx, 4)) return MOA_EINVAL;
-  st = check_workspace(workspace, workspace_bytes,
-                       attend4_chunks_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, n_chunks, max_ctx));
+  size_t need = 0;
+  st = moa_kv_attend_chunks_bytes(c, n_rows, n_chunks, max_ctx, &need);
+  if (st == MOA_OK) st = check_workspace(workspace, workspace_bytes, need);
   if (st != MOA_OK) return st;
   Attend4Args a = attend_args(c, kv, layer, q, type, q_stride, n_rows, tables, n_chunks, table_len, max_ctx, scale, out);
   a.chunk_start = chunk_start;
@@ -194,7 +211,7 @@ moa_status moa_kv_attend_chunks(const moa_kv_cfg* c, const void* kv, int32_t lay
 }
 
 moa_status moa_score_tokens_bytes(int32_t n_rows, int32_t vocab, int32_t top_k, size_t* bytes) {
-  if (n_rows < 0 || vocab < 1 || top_k < 0 || top_k > MOA_MAX_TOP || top_k > vocab || !bytes) return MOA_EINVAL;
+  if (n_rows < 0 || n_rows > kMaxRows || vocab < 1 || vocab > kMaxVocab || top_k < 0 || top_k > MOA_MAX_TOP || top_k > vocab || !bytes) return MOA_EINVAL;
   *bytes = score_bytes(n_rows, vocab, top_k);
   return MOA_OK;
 }

@@ -1,9 +1,10 @@
 """The cache and head operators on torch tensors: the C ABI's moa_kv_* and moa_score_tokens.
 
 Tensors live on one GPU; the work goes to torch's current stream of that GPU, results and workspaces come from torch's
-allocator, and nothing waits, so the calls can be captured into a graph. Arguments that do not fit are refused with
-ValueError before anything is launched; index tensors are read on the GPU (include/moa.h says what an entry that is out
-of range does). There is no fallback: without the built library or a GPU the calls raise.
+allocator, and nothing waits, so the calls can be captured into a graph. Arguments that do not fit are refused before
+anything is launched, with ValueError (tensors) or MoaError (sizes that the library refuses); index tensors are read on
+the GPU (include/moa.h says what an entry that is out of range does). These are operators of inference: no gradient
+passes through them. There is no fallback: without the built library or a GPU the calls raise.
 """
 import ctypes as C
 import math

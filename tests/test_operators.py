@@ -31,7 +31,7 @@ def q4(x):
     """(values, codes, scale, min) of the 4-bit rows of x (float32) along its last axis."""
     x = x.float()
     lo, hi = x.amin(-1, keepdim=True), x.amax(-1, keepdim=True)
-    m, s = lo.to(B), ((hi - lo) / 15).to(B)
+    m, s = lo.to(B), ((hi - lo) * torch.tensor(1 / 15, dtype=F)).to(B)
     bad = ~(x.isfinite().all(-1, keepdim=True) & (hi - lo).isfinite() & m.isfinite())
     s = torch.where(bad, torch.tensor(math.nan, dtype=B), s)
     m = torch.where(bad, torch.tensor(0.0, dtype=B), m)
@@ -251,6 +251,32 @@ def test_the_torch_layer_refuses_wrong_tensors(ops):
         ops.score_tokens(torch.zeros(2, 8, device="cuda"), z, top_k=9)
 
 
+@pytest.mark.parametrize("name", sorted(REFUSED))
+def test_sizes_past_the_grids_are_refused(name):
+    base = dict(REFUSED[name][0])
+    wrong = [dict(rows=(1 << 20) + 1)]
+    if name == "moa_score_tokens":
+        wrong += [dict(rows=1, vocab=(1 << 30) + 1, stride=1 << 31)]
+    else:
+        wrong += [dict(rows=1, table_len=(1 << 26) + 1), dict(rows=1, n_seqs=(1 << 20) + 1)]
+    if "max_ctx" in base:
+        wide = dict(KV, n_heads=512, n_kv_heads=512)
+        wrong += [dict(cfg=wide, stride=512 * 128, rows=1 << 20, n_seqs=1 << 20), dict(rows=1, table_len=1 << 26, max_ctx=(1 << 30) + 1)]
+    for w in wrong:
+        assert _c(name, dict(base, **w)) == M.MOA_EINVAL, w
+
+
+def test_sizes_past_64_bits_are_refused():
+    n = C.c_size_t()
+    top = (1 << 31) - 1
+    assert M.lib().moa_kv_bytes(C.byref(M.moa_kv_cfg(2, top, top, 4096, 4096, 128)), C.byref(n)) == M.MOA_EINVAL
+    cfg = C.byref(M.moa_kv_cfg(**KV))
+    assert M.lib().moa_kv_attend_bytes(cfg, 1, top, C.byref(n)) == M.MOA_EINVAL
+    assert M.lib().moa_kv_attend_chunks_bytes(cfg, 1, 1, top, C.byref(n)) == M.MOA_EINVAL
+    assert M.lib().moa_kv_attend_chunks_bytes(cfg, 1, top, 64, C.byref(n)) == M.MOA_EINVAL
+    assert M.lib().moa_score_tokens_bytes(1, top, 5, C.byref(n)) == M.MOA_EINVAL
+
+
 # ------------------------------------------------------------------ append and read
 
 def rows_of(lens, before, seed=0):
@@ -347,6 +373,50 @@ def test_rows_that_are_hard_to_quantise(ops, hd):
 
 
 @gpu
+@pytest.mark.parametrize("rows", [3, 512])
+def test_scales_next_to_a_border(ops, rows):
+    """Ranges whose 15th part lies between two bf16 values, where one bit of it decides."""
+    g = torch.Generator().manual_seed(2)
+    step = (torch.randint(128, 256, (rows,), generator=g) + 0.5) * 2.0 ** torch.randint(-9, -5, (rows,), generator=g).double()
+    hi = (step * 15).float()
+    for k in range(3):                                           # the nearest floats as well
+        x = torch.rand(rows, 3, 64, generator=g) * hi[:, None, None]
+        x[:, :, 5], x[:, :, 9] = 0.0, hi[:, None]
+        kv = ops.PagedKV("int4", 1, -(-rows // 16), 1, 1, 64)
+        tab = i32([range(-(-rows // 16))])
+        kv.append(0, x.flatten(1).cuda(), i32([0] * rows), i32(range(rows)), tab)
+        s = q4(x)[2][..., 0].view(torch.int16)
+        got = kv.pool.cpu().view(-1, 64 * 16 + 128)[:, 1024:].contiguous().view(torch.int16).view(-1, 2, 16, 2)[..., 0]
+        got = got.transpose(0, 1).reshape(2, -1)[:, :rows]
+        assert torch.equal(got[0], s[:, 1]) and torch.equal(got[1], s[:, 2])
+        hi = torch.nextafter(hi, torch.full_like(hi, math.inf))
+
+
+@gpu
+@pytest.mark.parametrize("hd,rows", [(64, 1), (128, 1), (64, 16), (128, 16)])
+def test_codes_next_to_a_border(ops, hd, rows):
+    """Values 2^-20 to 2^-29 of a step below and above the border of two codes, and on it (m = -2.75, s = 1.1015625)."""
+    kv = ops.PagedKV("int4", 1, 1, 1, 1, hd)
+    x = torch.zeros(rows, 3, hd, dtype=torch.float64)
+    i = torch.arange(hd, dtype=torch.float64)
+    for r in range(rows):
+        near = -2.75 + ((i % 14) + 0.5) * 1.1015625
+        near[2::14] *= 1 + (torch.arange(len(near[2::14])) - 2) * 2.0 ** (-12 - r % 10)     # 2.5 steps from m: next to 0, fine steps
+        near[0], near[-1] = -2.75, 13.75
+        x[r, 1:] = near
+    x = x.float().flatten(1)
+    kv.append(0, x.cuda(), i32([0] * rows), i32(range(rows)), i32([[0]]))
+    raw = kv.pool.cpu().numpy()
+    c, s, m = q4(x.view(rows, 3, hd)[:, 2])[1:]
+    assert float(s[0]) == 1.1015625 and float(m[0]) == -2.75 and len(c[0].unique()) > 8
+    vc = raw[8 * hd:16 * hd].reshape(hd // 2, 16)[:, :rows].T
+    kc = raw[:8 * hd].reshape(16, hd // 2)[:rows]
+    for r in range(rows):
+        assert np.concatenate([vc[r] & 15, vc[r] >> 4]).tolist() == c[r].tolist(), r
+        assert np.stack([kc[r] & 15, kc[r] >> 4], 1).reshape(-1).tolist() == c[r].tolist(), r
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["bf16", "int4"])
 def test_rows_out_of_range_are_skipped(ops, kind):
     hd, nh, nkv = 64, 2, 1
@@ -424,6 +494,30 @@ def test_decode_rows_with_sharp_scores(ops, hd):
     for r in range(5):
         want, A = attention(q[r].double(), p.k[0], p.v[0], hd ** -0.5)
         check_out(got[r], want, A, float(p.v[0].abs().max()), F, f"sharp row {r}")
+
+
+@gpu
+@pytest.mark.parametrize("q_size,scale", [(1e-42, 0.125), (1e-30, 1e-20), (1.0, 1e-44), (1.0, 0.0), (1.0, -0.125), (1e30, 1e-30)])
+def test_units_of_tiny_queries_and_scales(ops, q_size, scale):
+    """Subnormal queries, scales that leave no unit in float32, none and a negative one."""
+    p = Pool(ops, [100], 1, 2, 64, seed=9)
+    q = torch.randn(3, 2, 64, generator=torch.Generator().manual_seed(5)) * q_size
+    vm = float(p.v[0].abs().max())
+    for out, seen in ((p.kv.attend(0, q.cuda(), i32([0, 0, 0]), i32([98, 99, 100]), p.tables, 100, scale=scale), (98, 99, 100)),
+                      (p.kv.attend_chunks(0, q.cuda(), i32([0, 3]), i32([100]), p.tables, 100, scale=scale), (98, 99, 100))):
+        for r, n in enumerate(seen):
+            want, A = attention(q[r].double(), p.k[0][:n], p.v[0][:n], scale)
+            check_out(out[r], want, A, vm, F, f"q {q_size} scale {scale} row {r}")
+
+
+@gpu
+def test_chunk_starts_that_do_not_ascend_stay_inside(ops):
+    p = Pool(ops, [60, 60, 60], 1, 4, 64, seed=9)
+    whole = torch.full((200, 4, 64), 2.5, device="cuda")
+    q = torch.randn(70, 4, 64, generator=torch.Generator().manual_seed(5)).cuda()
+    for starts in ([0, 50, 20, 70], [60, 0, 65, 3], [70, 70, -5, 300]):
+        p.kv.attend_chunks(0, q, i32(starts), i32([60, 60, 60]), p.tables, 60, out=whole[60:130])
+    assert (whole[:60] == 2.5).all() and (whole[130:] == 2.5).all()
 
 
 @gpu
