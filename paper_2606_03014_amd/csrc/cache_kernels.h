@@ -14,6 +14,14 @@ __device__ __forceinline__ int kv_block(const KvPlace& p, int key, int pos) {
   return (unsigned)b < (unsigned)p.num_blocks ? b : -1;
 }
 
+// The row of workgroup b of T, for 4-bit cells: the 16 rows of a block share V's lines, a byte each, and
+// an XCD's L2 joins only what its own workgroups touch. Every eighth workgroup goes to one XCD, so it
+// gets 16 neighbours of each 128 rows (18,432 rows appended at 8 KV heads of 128: 148 -> 137 us, 2,048
+// rows 20.3 -> 18.8; read back 30.8 -> 27).
+__device__ __forceinline__ int row_of(int b, int T) {
+  return (b | 127) < T ? (b & ~127) + (b & 7) * 16 + ((b >> 3) & 15) : b;
+}
+
 // A cross-lane move of a double: its two words.
 template <int CTRL>
 __device__ __forceinline__ double dpp(double v) {
@@ -162,6 +170,11 @@ __device__ __forceinline__ void store_row(unsigned char* cell, int slot, bool v,
 // Keys of a 4-bit cache are computed in 64 bits: their codes are then
 // those of the float32 value, whatever the order of the norm's sum (one bit of the
 // float32 value can move the row's bf16 minimum, and with it every code).
+// Bound by bytes, and in 4-bit pools by the arithmetic in 64 bits and V's single bytes. 32 + 2 * 8 heads: 15,347
+// float32 rows (64 wide) into a bf16 pool 68 us, 5.0 TB/s; 18,348 bf16 rows (128 wide) into a 4-bit one
+// 141 us, 2.8 TB/s (their queries alone 72, 4.2 TB/s); 512 float32 rows 7.7 us. A wave for each run of
+// rows of one block, V in words, was slower up to 18k rows (157 us at 18,432, 66 against 57 at 8,192) and
+// 5 to 15% faster only at 65,536.
 
 // Lane l's dims of a head of row t.
 template <bool XBF, int HD, int N>
@@ -237,12 +250,13 @@ __device__ __forceinline__ void norm_rotate(const AppendArgs& a, const float g[N
   for (int i = 0; i < N; ++i) x[i] = (float)y[i];
 }
 
-// A workgroup is one row's next 256 / LP heads of the first `heads`: its position and block are scalars.
+// A workgroup is one row's next 256 / LP heads: its position and block are scalars.
 template <bool XBF, int KIND, int HD, bool NORM>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int heads, bool aligned) {
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, bool aligned) {
   constexpr int N = XBF ? 16 : 8, LP = HD / N;
-  const int t = blockIdx.x, l = threadIdx.x % LP, head = blockIdx.y * (256 / LP) + threadIdx.x / LP;
-  if (head >= heads) return;
+  const int t = KIND == KV_INT4 ? row_of(blockIdx.x, a.T) : blockIdx.x, l = threadIdx.x % LP;
+  const int head = blockIdx.y * (256 / LP) + threadIdx.x / LP;
+  if (head >= a.n_h + 2 * a.n_kv) return;
   float x[N], g[N], c[N];
   load_head<XBF, HD, N>(a, aligned, t, head, l, x);
   const bool is_q = head < a.n_h, is_v = head >= a.n_h + a.n_kv;
@@ -265,89 +279,15 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int heads, bool
   store_row<HD, KIND, N>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x, l);
 }
 
-// The keys and values of rows that follow one another in their sequences, into 4-bit cells:
-// a wave is a run of rows of one block (at most 16) and a KV head, so that a dim of V, whose 16 slots
-// lie side by side, is written in words instead of single bytes (prompts of 18k rows in all, 8 KV
-// heads of 128: 170 us byte by byte, with the queries).
-// A workgroup looks for the runs that begin in its 16 rows; its waves are four heads' keys or values.
-template <bool XBF, int HD, bool NORM>
-__global__ __launch_bounds__(256) void k_kv_append_runs(AppendArgs a, bool aligned) {
-  constexpr int LP = HD / 8, NR = 64 / LP, NI = 16 / NR;     // rows at a time, slots per group of lanes
-  const int lane = threadIdx.x & 63, l = lane % LP, rg = lane / LP;
-  const int unit = blockIdx.y * 4 + (threadIdx.x >> 6), t0 = blockIdx.x * 16;
-  if (unit >= 2 * a.n_kv) return;
-  const bool is_v = unit >= a.n_kv;
-  const int kh = is_v ? unit - a.n_kv : unit;
-  // lane i looks at row t0 - 1 + i; a row that follows the one before it in the same block is no beginning
-  const int ti = t0 - 1 + lane;
-  const bool there = ti >= 0 && ti < a.T;
-  const int pi = there ? a.row_pos[ti] : -2, ki = there ? a.place.key[ti] : -1;
-  const int pp = __shfl_up(pi, 1, 64), kp = __shfl_up(ki, 1, 64);
-  const bool follows = lane > 0 && pp >= 0 && pi == pp + 1 && (pi & 15) != 0 && ki == kp;
-  const unsigned long long chain = __ballot(follows);
-  unsigned long long begin = __ballot(lane >= 1 && lane <= 16 && pi >= 0 && !follows);
-  while (begin) {
-    const int j = __builtin_ctzll(begin);
-    begin &= begin - 1;
-    const int t1 = t0 - 1 + j, p1 = __builtin_amdgcn_readlane(pi, j), s0 = p1 & 15;
-    const int n = 1 + __builtin_ctzll(~(chain >> (j + 1)));  // rows; the block ends them, so rows t0 - 1 .. t0 + 30 tell
-    const int block = kv_block(a.place, __builtin_amdgcn_readlane(ki, j), p1);
-    float x[NI][8];
-    bool live[NI], whole = true;
-#pragma unroll
-    for (int it = 0; it < NI; ++it) {
-      const int i = rg * NI + it - s0;
-      live[it] = i >= 0 && i < n && !(a.rope && p1 + i >= a.rope_len);
-      whole = whole && live[it];
-      load_head<XBF, HD, 8>(a, aligned, live[it] ? t1 + i : t1, a.n_h + (is_v ? a.n_kv : 0) + kh, l, x[it]);
-    }
-    if (block < 0) continue;
-    unsigned char* cell = kv_cell(a.kv, KV_INT4, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh);
-    if (!is_v) {
-#pragma unroll
-      for (int it = 0; it < NI; ++it) {
-        const int slot = rg * NI + it, i = live[it] ? slot - s0 : 0;
-        float g[8], c[8];
-        if constexpr (NORM) load_gain<HD, 8>(a, a.k_gain, t1 + i, l, g);
-        if (a.rope) load_turn<HD, 8>(a, min(p1 + i, a.rope_len - 1), l, c);
-        norm_rotate<double, HD, 8, NORM>(a, g, c, x[it]);
-        if (live[it]) store_row<HD, KV_INT4, 8>(cell, slot, false, x[it], l);
-      }
-      continue;
-    }
-    unsigned word[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int it = 0; it < NI; ++it) {
-      int c[8];
-      const unsigned sc = quantise<HD, 8>(x[it], c);
-      if (live[it] && l == 0) ((unsigned*)(cell + 16 * HD))[16 + rg * NI + it] = sc;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) word[i] |= (unsigned)(c[i] | (c[i + 4] << 4)) << (8 * it);
-    }
-    unsigned char* vp = cell + 8 * HD + 4 * l * 16 + rg * NI;
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (NI == 4) *(unsigned*)(vp + i * 16) = word[i];
-        else *(uint16_t*)(vp + i * 16) = (uint16_t)word[i];
-      }
-    } else {
-#pragma unroll
-      for (int it = 0; it < NI; ++it)
-        if (live[it])
-#pragma unroll
-          for (int i = 0; i < 4; ++i) vp[i * 16 + it] = (unsigned char)(word[i] >> (8 * it));
-    }
-  }
-}
-
 // ------------------------------------------------- what cached positions hold
+// hd / 8 lanes a row. Bound by bytes and, in 4-bit cells, by V's single bytes: 18,348 rows of 8 heads of 128 27 us (95 MB).
 template <int KIND, int HD>
 __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, int layer, int n_kv, int T,
                                                  const int* __restrict__ row_pos, int pos0, KvPlace place,
                                                  void* __restrict__ kout, void* __restrict__ vout) {
   constexpr int LP = HD / 8;
-  const int t = blockIdx.x, l = threadIdx.x % LP, kh = blockIdx.y * (256 / LP) + threadIdx.x / LP;
+  const int t = KIND == KV_INT4 ? row_of(blockIdx.x, T) : blockIdx.x, l = threadIdx.x % LP;
+  const int kh = blockIdx.y * (256 / LP) + threadIdx.x / LP;
   if (kh >= n_kv) return;
   const int pos = row_pos ? row_pos[t] : pos0 + t, block = kv_block(place, place.key ? place.key[t] : 0, pos), slot = pos & 15;
   const size_t o = ((size_t)t * n_kv + kh) * HD;
@@ -403,6 +343,11 @@ __global__ __launch_bounds__(256) void k_kv_read(const void* __restrict__ kv, in
 // The softmax's reference M is kept so that p s_v stays below 2^13 (float16 holds it) and is
 // moved, with everything that was summed, only when a product passes that; p alone
 // may be as large as 2^98 then (tiny scales), which float32 sums hold.
+//
+// Bound by reading the cells, non-temporal, once: 384 rows of 1,000 to 8,000 keys, 32 heads of 128 over 8 KV
+// heads, bf16, 265 us, 5.3 TB/s; 7 float32 rows of 12,000 to 32,000 keys 41 us (3.8 TB/s: the join, the
+// start and the grid's tail); 160 of 64 to 3,000 at heads of 64 34 us. Three waves a SIMD hold a tile of keys and
+// one of values in registers; four spill (450 us), and double buffers gain nothing over non-temporal single ones.
 constexpr int kSplit4Max = 2048;
 constexpr unsigned kCodeMask = 0x00F000F0u;
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
@@ -746,10 +691,14 @@ __global__ __launch_bounds__(256) void k_attend4_join(Attend4Args a, int split, 
 // Tiles of 64 keys are unpacked once for the four waves: each thread brings 16 bytes of K
 // codes and 16 of V, a tile ahead of its unpacking and two ahead of their use, and
 // writes them as float16 codes (as in k_attend4_rows) to LDS in the order of the MFMA
-// operands, where V's [dim][slot] cells need no transposing. Two LDS buffers each. S^T = K Q^T: row 8 a + 4 h + i of a 32-key score tile is block a / 2, slot
-// 8 h + 4 (a % 2) + i, so lane half h ends with slots 8 h .. + 8 of both blocks, the k-slots of
-// O^T = V^T P^T. Scales, minima, the reference M and float16 pairs as in k_attend4_rows;
+// operands, where V's [dim][slot] cells need no transposing. Two LDS buffers each. S^T = K Q^T:
+// row 8 a + 4 h + i of a 32-key score tile is block a / 2, slot 8 h + 4 (a % 2) + i, so lane half h ends with
+// slots 8 h .. + 8 of both blocks, the k-slots of O^T = V^T P^T. Scales, minima, the reference M and float16 pairs as in k_attend4_rows;
 // in bf16 calls q is one exact float16 and P one float16, half the products.
+// Bound by the matrix cores and the VALU in turn. Float32, 32 heads of 128 over 8 KV heads, two chunks of
+// 1,501 to 4,096 rows behind 1,001 to 8,000 keys: 817 us, 508 TFLOP/s of useful products (twice that issued);
+// bf16, heads of 64, 24 prompts of 64 to 3,001 rows: 311 us, 370 TFLOP/s. Before a subtile's softmax ran
+// beside the next one's products: 873 and 369 us.
 struct Chunk { int row0, nq, pos0; const int* tab; };
 
 // The block of 128 / gq rows that workgroup slot b stands for: chunk i has the slots
@@ -1104,21 +1053,14 @@ hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendA
     a.gain_vec = a.gain_vec && (uintptr_t)a.q_gain.p[i] % 16 == 0 && (uintptr_t)a.k_gain.p[i] % 16 == 0;
   const size_t el = x_bf16 ? 8 : 4;                  // elements per 16 bytes
   const bool aligned = a.stride % el == 0 && a.split_stride % el == 0 && (uintptr_t)a.x % 16 == 0;
-  const int all = a.n_h + 2 * a.n_kv, heads = a.runs && kind == KV_INT4 ? a.n_h : all;
   const int wg = 256 * (x_bf16 ? 16 : 8) / a.hd;      // heads per workgroup
-  const dim3 grid(a.T, (heads + wg - 1) / wg), blk(256);
+  const dim3 grid(a.T, (a.n_h + 2 * a.n_kv + wg - 1) / wg), blk(256);
   const bool norm = a.q_gain.p[0] != nullptr;
   auto go = [&](auto bf, auto hd, auto k) {
     constexpr bool B = decltype(bf)::value;
     constexpr int D = decltype(hd)::value, K = decltype(k)::value;
-    if constexpr (K == KV_INT4)
-      if (heads < all) {
-        const dim3 tiles((a.T + 15) / 16, (2 * a.n_kv + 3) / 4);
-        if (norm) klaunch(k_kv_append_runs<B, D, true>, tiles, blk, st, a, aligned);
-        else klaunch(k_kv_append_runs<B, D, false>, tiles, blk, st, a, aligned);
-      }
-    if (norm) klaunch(k_kv_append<B, K, D, true>, grid, blk, st, a, heads, aligned);
-    else klaunch(k_kv_append<B, K, D, false>, grid, blk, st, a, heads, aligned);
+    if (norm) klaunch(k_kv_append<B, K, D, true>, grid, blk, st, a, aligned);
+    else klaunch(k_kv_append<B, K, D, false>, grid, blk, st, a, aligned);
     return hipGetLastError();
   };
   auto by_kind = [&](auto bf, auto hd) {

@@ -1267,7 +1267,7 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     const ReduceItem* red;
     const PrefillItem* pre;
     int nitems, nred, npre, max_item_blocks, pre_max_keys;
-    double attn_bytes, attn_flops, pre_bytes, pre_flops, red_bytes, pre_rows;
+    double attn_bytes, attn_flops, pre_bytes, pre_flops, red_bytes;
     int prev_split;
     size_t prev_stride;
   };
@@ -1309,7 +1309,6 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
     for (int i = d0; i < d0 + b.nred; ++i) nsl += e->red[i].nslots;
     b.pre_bytes = pre_keys * nkv * key_bytes + pre_rows * nh * hd * 8.0;
     b.pre_flops = pre_pairs * nh * hd * 4.0;
-    b.pre_rows = pre_rows;
     b.attn_bytes = kv_keys * nkv * key_bytes + (double)b.nr * nh * hd * 8.0;
     b.attn_flops = kv_keys * nh * hd * 4.0;
     b.red_bytes = nsl * nh * (hd + 2) * 4.0;
@@ -1428,7 +1427,6 @@ moa_status enqueue_step(moa_engine* e, const std::vector<int64_t>& admitted, int
             ap.n_kv = nkv;
             ap.hd = hd;
             ap.T = b.nr;
-            ap.runs = 2.0 * b.pre_rows > b.nr;
             LAUNCH(MOA_K_ROPE_KV, rope_bytes, 0, launch_kv_append(st, false, kind, ap), "kv append");
           } else {
             LAUNCH(MOA_K_ROPE_KV, rope_bytes, 0,

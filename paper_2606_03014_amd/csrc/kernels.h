@@ -212,7 +212,6 @@ struct AppendArgs {
   void* q;                 // [T][n_h][hd]
   void* kv;
   int layer, n_h, n_kv, hd, T;
-  bool runs;               // most rows follow the row before them in their sequence
 };
 // x_bf16: rows and q are bf16 (else f32).
 hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendArgs& a);

@@ -141,7 +141,6 @@ moa_status moa_kv_append(const moa_kv_cfg* c, void* kv, int32_t layer, const voi
   a.n_kv = c->n_kv_heads;
   a.hd = c->head_dim;
   a.T = n_rows;
-  a.runs = n_rows >= 4ll * n_seqs;         // prompts; decode rows stand alone
   return status_of(launch_kv_append((hipStream_t)hip_stream, type == MOA_BF16, c->kind, a), "moa_kv_append");
 }
 

@@ -22,6 +22,7 @@ __device__ __forceinline__ bool before(float a, int ia, float b, int ib) {
 //    came to it.
 //  * Rows whose list would not hold them (a thousand equal logits) or that hold NaN beside too
 //    few possible tokens search for one alternative after the other.
+// 512 rows of 128,256 float32 logits, 20 alternatives: 51 us, 5.2 TB/s (47 without alternatives).
 // Rows of any alignment are read in 16-byte pieces from the last 16-byte boundary on (such
 // a piece is inside the row's pages); what lies outside the row counts as -inf.
 constexpr int kScoreList = 1024, kScoreStep = 16384;   // list entries; logits per step
