@@ -1012,33 +1012,35 @@ __global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const 
   if (part.ml && hf == 0) *(float2*)(part.ml + 2 * prow) = make_float2(M, l);
 }
 
-// The join of a chunk's splits, in their order: a workgroup per block of rows and KV head.
+// The join of a chunk's splits, in their order: hd / 4 threads a row and head, workgroups of 1,024 / hd of
+// a block's 128 (all of them in one workgroup took 16 rows one after the other, each a chain of loads).
 template <int HD>
 __global__ __launch_bounds__(256) void k_attend4_chunks_join(Attend4Args a, int nsplit, Partial4 part) {
   const int gq = a.n_h / a.n_kv, PB = 128 / gq;
   const Chunk c = find_chunk(a, blockIdx.x, PB);
-  constexpr int TR = HD / 4;                       // threads a row and head
-  for (int i = threadIdx.x / TR; i < c.nq * gq; i += 256 / TR) {
-    const size_t row = (size_t)(c.row0 + i / gq) * a.n_h + blockIdx.y * gq + i % gq;
-    const int d = threadIdx.x % TR * 4;
-    float M = -INFINITY, l = 0.f;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < nsplit; ++s) {
-      const size_t b = (size_t)s * a.T * a.n_h + row;
-      const float2 ml = *(const float2*)(part.ml + 2 * b);
-      if (ml.x == -INFINITY) continue;             // nothing seen in this split: nothing was written
-      const f32x4_t as = *(const f32x4_t*)(part.acc + b * HD + d);
-      const float mn = fmaxf(M, ml.x), x = __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(ml.x - mn);
-      l = l * x + ml.y * y;
+  constexpr int TR = HD / 4;
+  const int i = blockIdx.z * (256 / TR) + threadIdx.x / TR, d = threadIdx.x % TR * 4;
+  if (i >= c.nq * gq) return;
+  const size_t row = (size_t)(c.row0 + i / gq) * a.n_h + blockIdx.y * gq + i % gq;
+  float M = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < nsplit; ++s) {
+    const size_t b = (size_t)s * a.T * a.n_h + row;
+    const float2 ml = *(const float2*)(part.ml + 2 * b);
+    const f32x4_t as = *(const f32x4_t*)(part.acc + b * HD + d);
+    const bool some = ml.x != -INFINITY;               // else nothing was seen in this split, and nothing written
+    const float mn = fmaxf(M, ml.x), x = M == mn ? 1.f : __builtin_amdgcn_exp2f(M - mn);
+    const float y = some ? __builtin_amdgcn_exp2f(ml.x - mn) : 0.f;
+    l = l * x + (some ? ml.y * y : 0.f);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = o[k] * x + as[k] * y;
-      M = mn;
-    }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] *= inv;
-    store_out4(a, row * HD + d, o);
+    for (int k = 0; k < 4; ++k) o[k] = o[k] * x + (some ? as[k] * y : 0.f);
+    M = mn;
   }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] *= inv;
+  store_out4(a, row * HD + d, o);
 }
 
 // =============================================================== launchers
@@ -1127,12 +1129,15 @@ hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* works
   return hipGetLastError();
 }
 
-// Workgroup slots and key splits of a chunk call: splits (of whole tiles, at least 512 keys)
-// only where the blocks of rows leave CUs without a workgroup.
+// Workgroup slots and key splits of a chunk call: splits (of whole tiles, at least 256 keys)
+// only where the blocks of rows make fewer than 512 workgroups, two a CU. us with that target at 256, 512,
+// 1,024 (bf16, 8 KV heads of 128, 4 query heads each): 128 rows behind 32,000 keys 192, 136, 149; 512 behind 8,000
+// 161, 119, 133; 2,048 behind 4,096 154, 154, 184; rows of 300, 40 and 900 behind 12,000 467, 445, 391. At
+// least 256, 512, 1,024 keys: 17 rows behind 8,000 31, 35, 50; 128 55, 55, 67.
 static void plan_chunks4(int n_h, int n_kv, int T, int n_chunks, int max_ctx, int& nslots, int& split, int& nsplit) {
   nslots = T / (128 / (n_h / n_kv)) + n_chunks;
   const long long wgs = (long long)nslots * n_kv;
-  nsplit = (int)std::max(1ll, std::min((512 + wgs - 1) / wgs, (long long)max_ctx / 512));
+  nsplit = (int)std::max(1ll, std::min((512 + wgs - 1) / wgs, (long long)max_ctx / 256));
   split = ((max_ctx + nsplit - 1) / nsplit + 63) / 64 * 64;
   nsplit = (max_ctx + split - 1) / split;
 }
@@ -1184,8 +1189,8 @@ hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* wor
   else a.q_bf16 ? go(k_attend4_chunks<128, false, false>) : go(k_attend4_chunks<128, false, true>);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || n == 1) return err;
-  if (a.hd == 64) klaunch(k_attend4_chunks_join<64>, dim3(nslots, a.n_kv), blk, st, a, n, part);
-  else klaunch(k_attend4_chunks_join<128>, dim3(nslots, a.n_kv), blk, st, a, n, part);
+  if (a.hd == 64) klaunch(k_attend4_chunks_join<64>, dim3(nslots, a.n_kv, 8), blk, st, a, n, part);
+  else klaunch(k_attend4_chunks_join<128>, dim3(nslots, a.n_kv, 16), blk, st, a, n, part);
   return hipGetLastError();
 }
 
