@@ -16,8 +16,8 @@ __device__ __forceinline__ int kv_block(const KvPlace& p, int key, int pos) {
 
 // The row of workgroup b of T, for 4-bit cells: the 16 rows of a block share V's lines, a byte each, and
 // an XCD's L2 joins only what its own workgroups touch. Every eighth workgroup goes to one XCD, so it
-// gets 16 neighbours of each 128 rows (18,432 rows appended at 8 KV heads of 128: 148 -> 137 us, 2,048
-// rows 20.3 -> 18.8; read back 30.8 -> 27).
+// gets 16 neighbours of each 128 rows (18,432 rows appended at 8 KV heads of 128: 137 us against 148, 2,048
+// rows 18.8 against 20.3; read back 27 against 30.8).
 __device__ __forceinline__ int row_of(int b, int T) {
   return (b | 127) < T ? (b & ~127) + (b & 7) * 16 + ((b >> 3) & 15) : b;
 }
@@ -166,15 +166,15 @@ __device__ __forceinline__ void store_row(unsigned char* cell, int slot, bool v,
 // ------------------------------ per-head norms, rotation and append in one pass
 // hd / N lanes hold one head of one row, each both halves of N / 2 rotation pairs, so
 // the norm's sum, the row's range and its codes stay within a row of 16 lanes; N = 8
-// values a lane in float32 and 16 in bf16 are 16-byte loads.
+// values a lane in float32 and 16 in bf16 are 16-byte loads. Rows of codes take 8 in bf16 too:
+// in 64 bits 16 need 80 registers, and fewer waves hide less (142 against 131 us for 18,348 rows).
 // Keys of a 4-bit cache are computed in 64 bits: their codes are then
 // those of the float32 value, whatever the order of the norm's sum (one bit of the
 // float32 value can move the row's bf16 minimum, and with it every code).
 // Bound by bytes, and in 4-bit pools by the arithmetic in 64 bits and V's single bytes. 32 + 2 * 8 heads: 15,347
 // float32 rows (64 wide) into a bf16 pool 68 us, 5.0 TB/s; 18,348 bf16 rows (128 wide) into a 4-bit one
-// 141 us, 2.8 TB/s (their queries alone 72, 4.2 TB/s); 512 float32 rows 7.7 us. A wave for each run of
-// rows of one block, V in words, was slower up to 18k rows (157 us at 18,432, 66 against 57 at 8,192) and
-// 5 to 15% faster only at 65,536.
+// 131 us, 3.0 TB/s (their queries alone 72, 4.2 TB/s); 512 float32 rows 7.3 us. A wave for each run of
+// rows of one block, V in words, was slower (18,432 rows 157 against 130 us, 8,192 66 against 54).
 
 // Lane l's dims of a head of row t.
 template <bool XBF, int HD, int N>
@@ -250,33 +250,48 @@ __device__ __forceinline__ void norm_rotate(const AppendArgs& a, const float g[N
   for (int i = 0; i < N; ++i) x[i] = (float)y[i];
 }
 
-// A workgroup is one row's next 256 / LP heads: its position and block are scalars.
+// Values a lane: of a query head (and of any head into f32 and bf16 cells), and of a key's or value's row of codes.
+constexpr int append_q_vals(bool xbf) { return xbf ? 16 : 8; }
+constexpr int append_kv_vals(bool xbf, int kind) { return kind == KV_INT4 ? 8 : append_q_vals(xbf); }
+
+// A workgroup is as many heads of one row as its threads hold, of queries or of keys and values:
+// its position and block are scalars.
 template <bool XBF, int KIND, int HD, bool NORM>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, bool aligned) {
-  constexpr int N = XBF ? 16 : 8, LP = HD / N;
-  const int t = KIND == KV_INT4 ? row_of(blockIdx.x, a.T) : blockIdx.x, l = threadIdx.x % LP;
-  const int head = blockIdx.y * (256 / LP) + threadIdx.x / LP;
-  if (head >= a.n_h + 2 * a.n_kv) return;
+  const int t = KIND == KV_INT4 ? row_of(blockIdx.x, a.T) : blockIdx.x;
+  {
+    constexpr int N = append_q_vals(XBF), LP = HD / N, HW = 256 / LP;
+    const int l = threadIdx.x % LP, head = blockIdx.y * HW + threadIdx.x / LP;
+    if (blockIdx.y * HW < a.n_h) {
+      if (head >= a.n_h) return;
+      float x[N], g[N], c[N];
+      load_head<XBF, HD, N>(a, aligned, t, head, l, x);
+      if (NORM) load_gain<HD, N>(a, a.q_gain, t, l, g);
+      const int pos = a.row_pos[t];
+      if (pos < 0 || (a.rope && pos >= a.rope_len)) return;
+      if (a.rope) load_turn<HD, N>(a, pos, l, c);
+      norm_rotate<float, HD, N, NORM>(a, g, c, x);
+      store_part<HD, N>(a.q, XBF, ((size_t)t * a.n_h + head) * HD, l, x);
+      return;
+    }
+  }
+  constexpr int N = append_kv_vals(XBF, KIND), LP = HD / N, HW = 256 / LP, QW = 256 * append_q_vals(XBF) / HD;
+  const int l = threadIdx.x % LP, kv = (blockIdx.y - (a.n_h + QW - 1) / QW) * HW + threadIdx.x / LP;
+  if (kv >= 2 * a.n_kv) return;
+  const bool is_v = kv >= a.n_kv;
   float x[N], g[N], c[N];
-  load_head<XBF, HD, N>(a, aligned, t, head, l, x);
-  const bool is_q = head < a.n_h, is_v = head >= a.n_h + a.n_kv;
-  if (NORM && !is_v) load_gain<HD, N>(a, is_q ? a.q_gain : a.k_gain, t, l, g);
+  load_head<XBF, HD, N>(a, aligned, t, a.n_h + kv, l, x);
+  if (NORM && !is_v) load_gain<HD, N>(a, a.k_gain, t, l, g);
   const int pos = a.row_pos[t];
   if (pos < 0 || (a.rope && pos >= a.rope_len)) return;
-  if (a.rope && !is_v) load_turn<HD, N>(a, pos, l, c);
-  if (is_q) {
-    norm_rotate<float, HD, N, NORM>(a, g, c, x);
-    store_part<HD, N>(a.q, XBF, ((size_t)t * a.n_h + head) * HD, l, x);
-    return;
-  }
   if (!is_v) {
+    if (a.rope) load_turn<HD, N>(a, pos, l, c);
     using T = std::conditional_t<KIND == KV_INT4, double, float>;
     norm_rotate<T, HD, N, NORM>(a, g, c, x);
   }
   const int block = kv_block(a.place, a.place.key[t], pos);
   if (block < 0) return;
-  const int kh = head - a.n_h - (is_v ? a.n_kv : 0);
-  store_row<HD, KIND, N>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, kh), pos & 15, is_v, x, l);
+  store_row<HD, KIND, N>(kv_cell(a.kv, KIND, HD, a.layer, a.place.num_blocks, block, a.n_kv, is_v ? kv - a.n_kv : kv), pos & 15, is_v, x, l);
 }
 
 // ------------------------------------------------- what cached positions hold
@@ -1055,8 +1070,8 @@ hipError_t launch_kv_append(hipStream_t st, bool x_bf16, int kind, const AppendA
     a.gain_vec = a.gain_vec && (uintptr_t)a.q_gain.p[i] % 16 == 0 && (uintptr_t)a.k_gain.p[i] % 16 == 0;
   const size_t el = x_bf16 ? 8 : 4;                  // elements per 16 bytes
   const bool aligned = a.stride % el == 0 && a.split_stride % el == 0 && (uintptr_t)a.x % 16 == 0;
-  const int wg = 256 * (x_bf16 ? 16 : 8) / a.hd;      // heads per workgroup
-  const dim3 grid(a.T, (a.n_h + 2 * a.n_kv + wg - 1) / wg), blk(256);
+  const int qw = 256 * append_q_vals(x_bf16) / a.hd, kw = 256 * append_kv_vals(x_bf16, kind) / a.hd;   // heads per workgroup
+  const dim3 grid(a.T, (a.n_h + qw - 1) / qw + (2 * a.n_kv + kw - 1) / kw), blk(256);
   const bool norm = a.q_gain.p[0] != nullptr;
   auto go = [&](auto bf, auto hd, auto k) {
     constexpr bool B = decltype(bf)::value;
