@@ -327,8 +327,9 @@ enum {
 /* Per-class launch statistics of the sampled steps. bytes/flops are the
  * algorithmic figures of those launches: for a GEMM the bf16 weights it
  * streams (N*K*2 per model group) plus its split-bf16 input (M*K*4) and fp32
- * output (M*N*4), flops 2*M*N*K; for attention the bf16 K/V it reads
- * (keys*2*head_dim*2 per KV head) plus q (fp32) and its output; for causal
+ * output (M*N*4), flops 2*M*N*K; for attention the K/V it reads
+ * (per KV head keys*4*head_dim in bf16, keys*(head_dim + 8) in 4 bits) plus
+ * q (fp32) and its output; token scores count under ARGMAX; for causal
  * prefill attention each block's keys once per KV head, and 4*head_dim flops
  * per (query head, query, visible key). */
 typedef struct {

@@ -789,6 +789,39 @@ def test_prompts_then_decode_then_scores(ops, hd, gq, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "int4"])
+def test_operands_of_any_alignment_give_the_same_bits(ops, dtype, kind):
+    """Views that begin one element behind a 16-byte boundary, with odd strides, against contiguous copies."""
+    hd, nkv, nh, T = 64, 2, 4, 40
+    g = torch.Generator().manual_seed(8)
+
+    def views(*shape):
+        x = torch.randn(shape[0], math.prod(shape[1:]) + 3, generator=g).to(dtype).cuda()
+        v = x[:, 1:-2]
+        assert v.data_ptr() % 16
+        return v, v.contiguous()
+
+    x, gains = views(T, (nh + 2 * nkv) * hd), [views(1, hd) for _ in range(2)]
+    seq, pos, tab, rope = i32([0] * T), i32(range(T)), i32([[2, 0, 1]]), ops.rope_table(T, hd)
+    got = []
+    for i in range(2):
+        kv = ops.PagedKV(kind, 1, 3, nh, nkv, hd)
+        got.append((kv.append(0, x[i], seq, pos, tab, rope=rope, q_gain=gains[0][i][0], k_gain=gains[1][i][0]), kv.pool))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    if kind != "int4":
+        return
+    q, c = views(T, nh * hd), i32([T])
+    outs = [(kv.attend(0, q[i].unflatten(1, (nh, hd)), seq, i32(range(1, T + 1)), tab, T),
+             kv.attend_chunks(0, q[i].unflatten(1, (nh, hd)), i32([0, T]), c, tab, T)) for i in range(2)]
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    v = views(3, 40001)
+    scores = [ops.score_tokens(v[i], i32([1, 2, 3]), top_k=9) for i in range(2)]
+    assert torch.equal(scores[0][2], scores[1][2])               # (sums run over other pieces: not their bits)
+    check_score(scores[0], score_want(v[1], i32([1, 2, 3]), 9))
+
+
+@gpu
 def test_calls_on_another_stream(ops):
     p = Pool(ops, [700, 90], 2, 4, 128, seed=2)
     q = torch.randn(2, 8, 128).cuda()
