@@ -468,8 +468,9 @@ moa_status moa_kv_attend(const moa_kv_cfg* cfg, const void* kv, int32_t layer, c
  * entries, within [0, n_rows]) and its last row is position chunk_ctx[i] - 1 of
  * the sequence of tables[i]; a row at position p sees keys [0, p], and one at
  * p < 0 is 0. Rows in no chunk are left as they were. Otherwise as
- * moa_kv_attend, with chunk_ctx[i] <= max_ctx (a chunk past it is clamped to
- * end at max_ctx). Chunks of any lengths may stand side by side, empty ones
+ * moa_kv_attend (the splits depend on n_rows, n_chunks, the heads, type and
+ * max_ctx), with chunk_ctx[i] <= max_ctx (a chunk past it is clamped to end
+ * at max_ctx). Chunks of any lengths may stand side by side, empty ones
  * too; single rows are what moa_kv_attend is for. */
 moa_status moa_kv_attend_chunks_bytes(const moa_kv_cfg* cfg, int32_t n_rows, int32_t n_chunks, int32_t max_ctx,
                                       size_t* bytes);

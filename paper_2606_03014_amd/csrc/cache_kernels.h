@@ -712,7 +712,7 @@ __global__ __launch_bounds__(256) void k_attend4_join(Attend4Args a, int split, 
 // in bf16 calls q is one exact float16 and P one float16, half the products.
 // Bound by the matrix cores and the VALU in turn. Float32, 32 heads of 128 over 8 KV heads, two chunks of
 // 1,501 to 4,096 rows behind 1,001 to 8,000 keys: 817 us, 508 TFLOP/s of useful products (twice that issued);
-// bf16, heads of 64, 24 prompts of 64 to 3,001 rows: 311 us, 370 TFLOP/s. Before a subtile's softmax ran
+// bf16, heads of 64, 24 prompts of 64 to 3,001 rows: 254 to 274 us, 420 to 450 TFLOP/s. Before a subtile's softmax ran
 // beside the next one's products: 873 and 369 us.
 struct Chunk { int row0, nq, pos0; const int* tab; };
 
@@ -750,8 +750,12 @@ __device__ __forceinline__ void store_out4(const Attend4Args& a, size_t at, f32x
   }
 }
 
+// Waves a SIMD: three of bf16 calls at heads of 64 (305 -> 274 us for the burst above); float32 ones spill
+// (560 -> 630 us for two long chunks), and 128 dims need the registers of two.
+constexpr int chunks4_waves(int hd, bool fine) { return hd == 64 && !fine ? 3 : 2; }
+
 template <int HD, bool ITEMS, bool FINE>
-__global__ __launch_bounds__(256, 2) void k_attend4_chunks(Attend4Args a, const PrefillItem* __restrict__ items, int nslots,
+__global__ __launch_bounds__(256, chunks4_waves(HD, FINE)) void k_attend4_chunks(Attend4Args a, const PrefillItem* __restrict__ items, int nslots,
                                                            int split, Partial4 part, bool q_vec) {
   constexpr int CELL = (int)kv_cell_bytes(KV_INT4, HD);
   constexpr int DS = HD / 16, DT = HD / 32;        // 16-dim steps of the scores, 32-dim tiles of the answer
@@ -1145,28 +1149,29 @@ hipError_t launch_attend4_rows(hipStream_t st, const Attend4Args& a, void* works
 }
 
 // Workgroup slots and key splits of a chunk call: splits (of whole tiles, at least 256 keys)
-// only where the blocks of rows make fewer than 512 workgroups, two a CU. us with that target at 256, 512,
-// 1,024 (bf16, 8 KV heads of 128, 4 query heads each): 128 rows behind 32,000 keys 192, 136, 149; 512 behind 8,000
-// 161, 119, 133; 2,048 behind 4,096 154, 154, 184; rows of 300, 40 and 900 behind 12,000 467, 445, 391. At
-// least 256, 512, 1,024 keys: 17 rows behind 8,000 31, 35, 50; 128 55, 55, 67.
-static void plan_chunks4(int n_h, int n_kv, int T, int n_chunks, int max_ctx, int& nslots, int& split, int& nsplit) {
-  nslots = T / (128 / (n_h / n_kv)) + n_chunks;
-  const long long wgs = (long long)nslots * n_kv;
-  nsplit = (int)std::max(1ll, std::min((512 + wgs - 1) / wgs, (long long)max_ctx / 256));
-  split = ((max_ctx + nsplit - 1) / nsplit + 63) / 64 * 64;
-  nsplit = (max_ctx + split - 1) / split;
+// only where the blocks of rows make fewer workgroups than run at once, two or three a CU. us with a target of
+// 256, 512, 1,024 (bf16, 8 KV heads of 128, 4 query heads each): 128 rows behind 32,000 keys 192, 136, 149; 512 behind
+// 8,000 161, 119, 133; 2,048 behind 4,096 154, 154, 184; rows of 300, 40 and 900 behind 12,000 467, 445, 391. At
+// least 256, 512, 1,024 keys: 17 rows behind 8,000 31, 35, 50; 128 55, 55, 67. Heads of 64, targets of 512 and
+// 768: 128 rows behind 32,000 102, 91; 1,024 behind 16,000 278, 244; 2,048 behind 4,096 116, 120.
+static void plan_chunks4(const Chunks4Size& z, bool bf16, int& nslots, int& split, int& nsplit) {
+  nslots = z.T / (128 / (z.n_h / z.n_kv)) + z.n_chunks;
+  const long long wgs = (long long)nslots * z.n_kv, target = 256 * chunks4_waves(z.hd, !bf16);
+  nsplit = (int)std::max(1ll, std::min((target + wgs - 1) / wgs, (long long)z.max_ctx / 256));
+  split = ((z.max_ctx + nsplit - 1) / nsplit + 63) / 64 * 64;
+  nsplit = (z.max_ctx + split - 1) / split;
 }
 
-bool attend4_chunks_fits(int n_h, int n_kv, int T, int n_chunks, int max_ctx) {
+bool attend4_chunks_fits(const Chunks4Size& z) {
   int nslots, split, n;
-  plan_chunks4(n_h, n_kv, T, n_chunks, max_ctx, nslots, split, n);
-  return (long long)nslots * n * n_kv <= kMaxGrid;
+  plan_chunks4(z, true, nslots, split, n);               // (the type with the most splits)
+  return (long long)nslots * n * z.n_kv <= kMaxGrid;
 }
 
-size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx) {
+size_t attend4_chunks_bytes(const Chunks4Size& z) {
   int nslots, split, n;
-  plan_chunks4(n_h, n_kv, T, n_chunks, max_ctx, nslots, split, n);
-  return n > 1 ? up256((size_t)n * T * n_h * hd * 4) + (size_t)n * T * n_h * 8 : 0;
+  plan_chunks4(z, true, nslots, split, n);
+  return n > 1 ? up256((size_t)n * z.T * z.n_h * z.hd * 4) + (size_t)n * z.T * z.n_h * 8 : 0;
 }
 
 static unsigned chunks4_lds(int hd) { return 4u * 64u * (unsigned)hd * 2u + 3u * 1024u; }
@@ -1190,7 +1195,7 @@ static hipError_t chunks4_attributes() {
 hipError_t launch_attend4_chunks(hipStream_t st, const Attend4Args& a, void* workspace) {
   if (a.T <= 0) return hipSuccess;
   int nslots, split, n;
-  plan_chunks4(a.n_h, a.n_kv, a.T, a.n_seqs, a.max_ctx, nslots, split, n);
+  plan_chunks4({a.n_h, a.n_kv, a.hd, a.T, a.n_seqs, a.max_ctx}, a.q_bf16, nslots, split, n);
   if ((a.hd != 64 && a.hd != 128) || a.n_h / a.n_kv > 8 || (long long)nslots * n * a.n_kv > kMaxGrid) return hipErrorInvalidValue;
   Partial4 part{nullptr, nullptr};
   if (n > 1) part = {(float*)workspace, (float*)((char*)workspace + up256((size_t)n * a.T * a.n_h * a.hd * 4))};

@@ -248,9 +248,10 @@ hipError_t launch_attend4_items(hipStream_t st, const Attend4Args& a, const Attn
 hipError_t launch_attend4_prefill(hipStream_t st, const Attend4Args& a, const PrefillItem* items, int nitems);
 // (fits: the call's grid can be launched)
 bool attend4_rows_fits(int n_kv, int T, int max_ctx);
-bool attend4_chunks_fits(int n_h, int n_kv, int T, int n_chunks, int max_ctx);
+struct Chunks4Size { int n_h, n_kv, hd, T, n_chunks, max_ctx; };
+bool attend4_chunks_fits(const Chunks4Size& z);
 size_t attend4_rows_bytes(int n_h, int n_kv, int hd, int T, int max_ctx);
-size_t attend4_chunks_bytes(int n_h, int n_kv, int hd, int T, int n_chunks, int max_ctx);
+size_t attend4_chunks_bytes(const Chunks4Size& z);       // for either type
 
 // Injected history into 4-bit cells (src: bf16; values as launch_kv_fill's, rounded to bf16).
 hipError_t launch_kv4_scatter(hipStream_t st, const void* src, void* kv, const int* blocks, int p0, int n, int layer,

@@ -185,8 +185,9 @@ moa_status moa_kv_attend_chunks_bytes(const moa_kv_cfg* c, int32_t n_rows, int32
   if (!valid_kv(c) || c->kind != MOA_KV_INT4 || n_rows < 0 || n_rows > kMaxRows || n_chunks < 1 || n_chunks > kMaxRows ||
       max_ctx < 1 || max_ctx > 16 * kMaxTable || !bytes)
     return MOA_EINVAL;
-  if (!attend4_chunks_fits(c->n_heads, c->n_kv_heads, n_rows, n_chunks, max_ctx)) return MOA_EINVAL;
-  *bytes = attend4_chunks_bytes(c->n_heads, c->n_kv_heads, c->head_dim, n_rows, n_chunks, max_ctx);
+  const Chunks4Size z{c->n_heads, c->n_kv_heads, c->head_dim, n_rows, n_chunks, max_ctx};
+  if (!attend4_chunks_fits(z)) return MOA_EINVAL;
+  *bytes = attend4_chunks_bytes(z);
   return MOA_OK;
 }
 
