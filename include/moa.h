@@ -469,7 +469,8 @@ moa_status moa_kv_attend(const moa_kv_cfg* cfg, const void* kv, int32_t layer, c
  * the sequence of tables[i]; a row at position p sees keys [0, p], and one at
  * p < 0 is 0. Rows in no chunk are left as they were. Otherwise as
  * moa_kv_attend (the splits depend on n_rows, n_chunks, the heads, type and
- * max_ctx), with chunk_ctx[i] <= max_ctx (a chunk past it is clamped to end
+ * max_ctx; between those the bits of a row hang on nothing but the row, so
+ * not on where its prompt is cut into chunks), with chunk_ctx[i] <= max_ctx (a chunk past it is clamped to end
  * at max_ctx). Chunks of any lengths may stand side by side, empty ones
  * too; single rows are what moa_kv_attend is for. */
 moa_status moa_kv_attend_chunks_bytes(const moa_kv_cfg* cfg, int32_t n_rows, int32_t n_chunks, int32_t max_ctx,

@@ -937,17 +937,19 @@ __global__ __launch_bounds__(256, chunks4_waves(HD, FINE)) void k_attend4_chunks
       for (int e = 16 * s / DS; e < 16 * (s + 1) / DS; ++e) probability(e, base);
       __builtin_amdgcn_sched_barrier(0);
     }
-    // the reference moves: at the first keys that a query meets, or past 2^13
+    // a query's reference moves at the first keys that it meets, or past 2^13: by its own scores alone,
+    // so that its bits do not hang on the rows beside it
     const int fine = __all(pm <= 8192.f && ts < INFINITY) & !__any(M == -INFINITY);
     if (!fine) {
       float u = -INFINITY, big = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         u = fmaxf(u, S[e]);
-        big = fmaxf(big, vc[(16 * (e >> 3) + (e & 7)) * 2]);
+        big = fmaxf(big, S[e] == -INFINITY ? 0.f : vc[(16 * (e >> 3) + (e & 7)) * 2]);   // of the keys that it sees
       }
       u = fmaf(max_halves(u), f, fmaxf(__builtin_amdgcn_logf(max_halves(big)), -90.f));
-      u = fmaxf(u - 8.f, M);
+      const bool stays = max_halves(pm) <= 8192.f && add_halves(ts) < INFINITY && M != -INFINITY;
+      u = stays ? M : fmaxf(u - 4.f, M);               // 2^9 from there to the next move, 2^-28 of the largest p s kept
       const float alpha = M == u ? 1.f : __builtin_amdgcn_exp2f(M - u);
       M = u;
       l *= alpha;

@@ -596,6 +596,21 @@ def test_a_nan_row_reaches_only_later_rows_of_a_chunk(ops, hd, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("hd,gq,spread", [(64, 4, 1.0), (128, 2, 3.0), (64, 1, 4.0), (128, 8, 1.0)])
+def test_chunk_bits_do_not_hang_on_the_cuts(ops, hd, gq, spread, dtype):
+    """One prompt whole, and cut at any row, in calls without key splits: the same bits, also where references move."""
+    n = 400
+    p = Pool(ops, [n], 1, gq, hd, seed=12, spread=spread)
+    q = (torch.randn(n, gq, hd, generator=torch.Generator().manual_seed(4)) * spread).to(dtype).cuda()
+    whole = p.kv.attend_chunks(0, q, i32([0, n]), i32([n]), p.tables, n)
+    for cuts in ([0, 150, n], [0, 1, 18, 83, 311, n]):
+        for a, b in zip(cuts, cuts[1:]):
+            part = p.kv.attend_chunks(0, q[a:b], i32([0, b - a]), i32([b]), p.tables, n)
+            assert torch.equal(part, whole[a:b]), (a, b)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F, B])
 @pytest.mark.parametrize("hd,gq", [(64, 4), (128, 2)])
 def test_few_rows_behind_long_contexts(ops, hd, gq, dtype):
     """Grids that are split over the keys: chunks whose first rows see none of the later splits, an empty one."""
